@@ -62,7 +62,7 @@ extern "C" {
 /* Raised with every change of a signature, a struct, the meaning of an argument or a
  * documented result; the Python binding refuses a library that reports another
  * version. */
-#define VC_JOINTATTN_ABI_VERSION 11
+#define VC_JOINTATTN_ABI_VERSION 12
 
 typedef enum vc_status {
   VC_OK = 0,
@@ -389,6 +389,123 @@ vc_status vc_offload_load(vc_offload* h, void* dev_dst, const void* host_src, si
 
 /* Makes `stream` wait (on the device) for every copy issued so far. */
 vc_status vc_offload_wait(vc_offload* h, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Packed attention: softmax attention of S sequences of different lengths laid one
+ * behind the other, as a text tower's captions come, or prompts, or one token each
+ * at the end of a long cache. Query rows [cu_q[s], cu_q[s+1]) of q and key rows
+ * [cu_k[s], cu_k[s+1]) of k and v are the slots of sequence s; the first len_q[s]
+ * (len_k[s]) rows of a slot take part, all of them where the array is NULL. Key head
+ * h / (heads / kv_heads) serves query head h. With n_q query and n_k key rows, query i
+ * stands at position p_i = i + n_k - n_q of the keys (the last query at the last key):
+ *
+ *   s_ij = c <q_i, k_j> + b_ij, valid for j < n_k and, with `causal`, j <= p_i,
+ *   b_ij = bias[h][buckets[R + clamp(j - p_i, -R, R)]], R = max_distance (0 without a
+ *   bias, and where the bucket is none of 0 .. num_buckets - 1),
+ *
+ * and LSE, O, dQ, dK, dV as above (dK, dV summed over the query heads of a group) and
+ * dbias[h][u] = the sum of dS_ij over the pairs of bucket u. A query that sees no key
+ * (causal, and more queries than keys; or shut out by the bias) gets O = 0, LSE = -inf,
+ * dQ = 0. An entry of the bias below -65536 (-inf, or a type's lowest value) shuts its
+ * pairs out: probability exactly 0; one above 65536 counts as 65536.
+ *  - q [total_q, heads, D], k, v [total_k, kv_heads, D]: bf16, 16-byte aligned, heads
+ *    contiguous, tokens q_stride (k_stride, v_stride) elements apart. o, dout, dq:
+ *    contiguous like q; dk, dv like k. lse: fp32 [heads, total_q].
+ *  - cu_q, cu_k: device int32 [S + 1], not decreasing; len_q, len_k: device int32 [S] or
+ *    NULL. They are read on the device only: an offset or length outside its tensor or slot
+ *    is taken as the nearest inside, a slot of more than max_q (max_k) rows as one of
+ *    that many.
+ *  - bias: bf16 [heads, num_buckets]; buckets: device int32 [2 R + 1]. Both NULL or
+ *    ignored with num_buckets = 0.
+ *  - Rows of a slot behind its length get O = 0, LSE = -inf, dQ = 0 (dK = dV = 0 exactly);
+ *    what q, k, v and dout hold there has no effect. Rows outside every slot are left as
+ *    they were, or with `clear_outside` written as those. Values of rows that take part must be
+ *    finite: a causal query's row is computed together with up to 63 later keys.
+ *  - Deterministic: no atomics; dK and dV of a key are summed in one order.
+ * ------------------------------------------------------------------------- */
+typedef struct vc_packedattn_desc {
+  int32_t sequences;      /* S >= 1                                             */
+  int32_t heads;          /* query heads, a multiple of kv_heads                */
+  int32_t kv_heads;       /* key and value heads                                */
+  int32_t head_dim;       /* D, 64 or 128                                       */
+  int64_t total_q;        /* rows of q, >= 1                                    */
+  int64_t total_k;        /* rows of k and v, >= 1                              */
+  int32_t max_q;          /* at least the rows of the longest query slot        */
+  int32_t max_k;          /* at least the rows of the longest key slot          */
+  int64_t q_stride;       /* elements between tokens, a multiple of 8; 0: heads * D */
+  int64_t k_stride;
+  int64_t v_stride;
+  int32_t causal;         /* 0 or 1                                             */
+  float softmax_scale;    /* c; <= 0 selects 1/sqrt(D). 2^-60 .. 2^60, with a bias 2^-24 .. 2^24 */
+  int32_t num_buckets;    /* 0: no bias; up to 1024                             */
+  int32_t max_distance;   /* R, 0 .. 512                                        */
+  int32_t clear_outside;  /* 1: outputs' rows outside every slot are written too */
+} vc_packedattn_desc;
+
+/* Bytes of device workspace of the forward and of the backward (the backward: per query
+ * row and head fp32 -LSE/c and -D, and the bias gradient's sums per distance); 0 for an
+ * invalid descriptor. Host only. */
+size_t vc_packedattn_fwd_workspace_bytes(const vc_packedattn_desc* desc);
+size_t vc_packedattn_bwd_workspace_bytes(const vc_packedattn_desc* desc);
+
+/* Packed forward: o and lse. `workspace`: caller-owned, at least the queried bytes, 256-byte
+ * aligned; its contents on entry do not matter. */
+vc_status vc_packedattn_fwd(const vc_packedattn_desc* desc,
+                            const void* q, const void* k, const void* v,
+                            const int32_t* cu_q, const int32_t* cu_k,
+                            const int32_t* len_q, const int32_t* len_k,
+                            const void* bias, const int32_t* buckets,
+                            void* o, float* lse,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* Packed backward: dq, dk, dv and, unless it is NULL, dbias (bf16 [heads, num_buckets])
+ * from the forward's o and lse and dout. */
+vc_status vc_packedattn_bwd(const vc_packedattn_desc* desc,
+                            const void* q, const void* k, const void* v,
+                            const void* o, const float* lse, const void* dout,
+                            const int32_t* cu_q, const int32_t* cu_k,
+                            const int32_t* len_q, const int32_t* len_k,
+                            const void* bias, const int32_t* buckets,
+                            void* dq, void* dk, void* dv, void* dbias,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Layer norm over the columns of each row, as stands before every attention:
+ * y = (x - mean) rstd w + b, rstd = 1 / sqrt(mean of (x - mean)^2 + eps), and backward,
+ * with g = dout w and xh = (x - mean) rstd,
+ *   dx = rstd (g - mean of g - xh (mean of g xh)), dw = sum over rows of dout xh,
+ *   db = sum over rows of dout.
+ * Sums in fp32, in a fixed order (no atomics). y, dx: contiguous, of x's type; mean and
+ * rstd: fp32 [rows]; weight, bias, dweight, dbias: [cols] of param_type. weight and bias
+ * may be NULL (1 and 0), dweight and dbias too (not wanted). Pointers aligned to their
+ * element.
+ * ------------------------------------------------------------------------- */
+#define VC_BF16 0
+#define VC_FP32 1
+
+typedef struct vc_layernorm_desc {
+  int64_t rows;           /* 1 .. 2^30                                          */
+  int32_t cols;           /* 1 .. 65536                                         */
+  int32_t x_type;         /* VC_BF16 or VC_FP32: x, y, dout, dx                 */
+  int32_t param_type;     /* VC_BF16 or VC_FP32: weight, bias and their gradients */
+  float eps;              /* >= 0                                               */
+  int64_t x_stride;       /* elements between the rows of x; 0: cols            */
+  int64_t dout_stride;    /* elements between the rows of dout; 0: cols         */
+} vc_layernorm_desc;
+
+vc_status vc_layernorm_fwd(const vc_layernorm_desc* desc,
+                           const void* x, const void* weight, const void* bias,
+                           void* y, float* mean, float* rstd, void* stream);
+
+/* Bytes of device workspace of the backward (partial column sums); 0 for an invalid
+ * descriptor. Host only. */
+size_t vc_layernorm_bwd_workspace_bytes(const vc_layernorm_desc* desc);
+
+vc_status vc_layernorm_bwd(const vc_layernorm_desc* desc,
+                           const void* dout, const void* x, const void* weight,
+                           const float* mean, const float* rstd,
+                           void* dx, void* dweight, void* dbias,
+                           void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -18,7 +18,7 @@ HEADER = os.path.join(os.path.dirname(PKG_DIR), "include", "vc_jointattn.h")
 # The ABI the signatures below describe (VC_JOINTATTN_ABI_VERSION of include/vc_jointattn.h);
 # a library reporting another version is refused, so that no call can reach an entry point
 # whose arguments differ from what this binding passes.
-ABI_VERSION = 11
+ABI_VERSION = 12
 # Bytes of the no-allocation forward's fixed scratch array (VC_JOINTATTN_NOALLOC_SCRATCH_BYTES).
 NOALLOC_SCRATCH_BYTES = 256 << 20
 
@@ -51,9 +51,44 @@ class vc_jointattn_desc(ctypes.Structure):
     ]
 
 
+class vc_packedattn_desc(ctypes.Structure):
+    _fields_ = [
+        ("sequences", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("total_q", ctypes.c_int64),
+        ("total_k", ctypes.c_int64),
+        ("max_q", ctypes.c_int32),
+        ("max_k", ctypes.c_int32),
+        ("q_stride", ctypes.c_int64),
+        ("k_stride", ctypes.c_int64),
+        ("v_stride", ctypes.c_int64),
+        ("causal", ctypes.c_int32),
+        ("softmax_scale", ctypes.c_float),
+        ("num_buckets", ctypes.c_int32),
+        ("max_distance", ctypes.c_int32),
+        ("clear_outside", ctypes.c_int32),
+    ]
+
+
+class vc_layernorm_desc(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int32),
+        ("x_type", ctypes.c_int32),
+        ("param_type", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("x_stride", ctypes.c_int64),
+        ("dout_stride", ctypes.c_int64),
+    ]
+
+
 _LIB = None
 _P = ctypes.c_void_p
 _DP = ctypes.POINTER(vc_jointattn_desc)
+_PP = ctypes.POINTER(vc_packedattn_desc)
+_NP = ctypes.POINTER(vc_layernorm_desc)
 _SIGS = {
     "vc_jointattn_abi_version": (ctypes.c_int, []),
     "vc_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -81,6 +116,13 @@ _SIGS = {
     "vc_offload_wait": (ctypes.c_int, [ctypes.c_void_p, _P]),
     "vc_temporalattn_bwd_workspace_bytes": (ctypes.c_size_t, [_DP]),
     "vc_temporalattn_bwd": (ctypes.c_int, [_DP, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "vc_packedattn_fwd_workspace_bytes": (ctypes.c_size_t, [_PP]),
+    "vc_packedattn_bwd_workspace_bytes": (ctypes.c_size_t, [_PP]),
+    "vc_packedattn_fwd": (ctypes.c_int, [_PP] + [_P] * 12 + [ctypes.c_size_t, _P]),
+    "vc_packedattn_bwd": (ctypes.c_int, [_PP] + [_P] * 17 + [ctypes.c_size_t, _P]),
+    "vc_layernorm_fwd": (ctypes.c_int, [_NP] + [_P] * 7),
+    "vc_layernorm_bwd_workspace_bytes": (ctypes.c_size_t, [_NP]),
+    "vc_layernorm_bwd": (ctypes.c_int, [_NP] + [_P] * 9 + [ctypes.c_size_t, _P]),
 }
 
 
@@ -562,3 +604,10 @@ def temporal_attention(q, k, v, desc, key_mask=None):
 def parallel_block_attention(q, k, v, desc, text_len=None, key_mask=None):
     """Differentiable sum of the joint, spatial and temporal branches on shared q, k, v."""
     return _autograd_functions()["block"].apply(q, k, v, desc, text_len, key_mask)
+
+
+# The text tower's operators (packed attention, layer norm).
+from .tower import (layer_norm, layer_norm_bwd, layer_norm_fwd, make_packed_desc, packed_attention,  # noqa: E402,F401
+                    packed_bwd, packed_bwd_workspace, packed_fwd, packed_fwd_workspace, relative_buckets,
+                    vc_layernorm_bwd, vc_layernorm_bwd_workspace_bytes, vc_layernorm_fwd, vc_packedattn_bwd,
+                    vc_packedattn_bwd_workspace_bytes, vc_packedattn_fwd, vc_packedattn_fwd_workspace_bytes)

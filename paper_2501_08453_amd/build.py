@@ -10,8 +10,9 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libvc_jointattn.so")
-SOURCES = ["api.hip", "layout.hip", "fwd.hip", "bwd.hip", "temporal.hip", "temporal_long.hip", "offload.hip"]
-HEADERS = ["common.hpp"]
+SOURCES = ["api.hip", "layout.hip", "fwd.hip", "bwd.hip", "temporal.hip", "temporal_long.hip", "offload.hip",
+           "api_tower.hip", "packed_fwd.hip", "packed_bwd.hip", "norm.hip"]
+HEADERS = ["common.hpp", "host.hpp", "packed.hpp", "norm.hpp"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

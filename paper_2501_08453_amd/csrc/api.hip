@@ -10,7 +10,7 @@
 #include <mutex>
 
 #include "common.hpp"
-#include "vc_jointattn.h"
+#include "host.hpp"
 
 namespace {
 
@@ -23,6 +23,9 @@ struct DeviceInfo {
 };
 DeviceInfo g_devices[kMaxDevices];
 
+}  // namespace
+
+namespace vcja {
 vc_status check_device() {
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return VC_ERR_DEVICE;
@@ -36,6 +39,19 @@ vc_status check_device() {
   });
   return di.is_gfx950 ? VC_OK : VC_ERR_DEVICE;
 }
+
+int device_cus() {
+  int dev = 0;
+  (void)hipGetDevice(&dev);
+  return g_devices[dev].cus;
+}
+}  // namespace vcja
+
+namespace {
+using vcja::aligned16;
+using vcja::aligned4;
+using vcja::check_device;
+using vcja::device_cus;
 
 // Workspace of vc_jointattn_fwd_noalloc: a file-scope device array (each device holds its
 // own copy from the library's first use on it until the process ends). In host code
@@ -62,15 +78,6 @@ void* scratch_ptr() {
   return sa.ptr;
 }
 
-// Compute units of the current device (after check_device succeeded).
-int device_cus() {
-  int dev = 0;
-  (void)hipGetDevice(&dev);
-  return g_devices[dev].cus;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // Validates a descriptor; on success fills N.
 vc_status check_desc(const vc_jointattn_desc* d, int64_t* n_out) {

@@ -1,0 +1,256 @@
+// Host side of the packed attention's and the layer norm's entry points: argument
+// validation, workspace layout, launches. Nothing here allocates, frees or synchronises.
+#include <math.h>
+
+#include <algorithm>
+
+#include "host.hpp"
+#include "norm.hpp"
+#include "packed.hpp"
+
+namespace {
+
+using vcja::aligned16;
+using vcja::aligned4;
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+inline hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
+inline const __bf16* bf(const void* p) { return static_cast<const __bf16*>(p); }
+
+constexpr int64_t kMaxRows = (int64_t)1 << 30;
+constexpr int64_t kMaxStride = (int64_t)1 << 23;  // elements between tokens: tile offsets of 16 rows stay in 32 bits
+
+int64_t stride_of(int64_t given, int64_t heads, int64_t d) { return given ? given : heads * d; }
+
+vc_status check_packed(const vc_packedattn_desc* d) {
+  if (!d) return VC_ERR_NULL;
+  if (d->head_dim != 64 && d->head_dim != 128) return VC_ERR_HEAD_DIM;
+  if (d->sequences < 1 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads) return VC_ERR_SHAPE;
+  if (d->sequences > (1 << 20) || d->heads > 4096) return VC_ERR_SHAPE;
+  if (d->total_q < 1 || d->total_q > kMaxRows || d->total_k < 1 || d->total_k > kMaxRows) return VC_ERR_SHAPE;
+  if (d->max_q < 1 || d->max_q > d->total_q || d->max_k < 1 || d->max_k > d->total_k) return VC_ERR_SHAPE;
+  if ((d->causal & ~1) || (d->clear_outside & ~1)) return VC_ERR_SHAPE;
+  const int64_t D = d->head_dim;
+  for (const int64_t s : {d->q_stride, d->k_stride, d->v_stride})
+    if (s < 0 || s > kMaxStride || s % 8) return VC_ERR_SHAPE;
+  if (stride_of(d->q_stride, d->heads, D) < d->heads * D || stride_of(d->k_stride, d->kv_heads, D) < d->kv_heads * D ||
+      stride_of(d->v_stride, d->kv_heads, D) < d->kv_heads * D)
+    return VC_ERR_SHAPE;
+  if (d->num_buckets < 0 || d->num_buckets > vcja::kMaxBuckets || d->max_distance < 0 || d->max_distance > vcja::kMaxBiasDistance)
+    return VC_ERR_SHAPE;
+  // Scores are formed in units of 1 / c; with a bias that quotient is taken of its entries too.
+  if (!(d->softmax_scale <= 0.0f)) {
+    const float c = d->softmax_scale, lo = d->num_buckets ? 0x1p-24f : 0x1p-60f, hi = d->num_buckets ? 0x1p24f : 0x1p60f;
+    if (!(c >= lo && c <= hi)) return VC_ERR_SHAPE;
+  }
+  // Row counts of the statistics and workgroup counts stay inside 32 bits.
+  const int64_t blocks = (int64_t)d->heads * d->sequences * ((std::max(d->max_q, d->max_k) + 31) / 32);
+  if (blocks > ((int64_t)1 << 30) || vcja::packed_rows(d->total_q, d->sequences) > ((int64_t)1 << 31) - 1) return VC_ERR_SHAPE;
+  return VC_OK;
+}
+
+float scale_of(const vc_packedattn_desc* d) {
+  return d->softmax_scale > 0.0f ? d->softmax_scale : 1.0f / sqrtf((float)d->head_dim);
+}
+
+vcja::PackedArgs packed_args(const vc_packedattn_desc* d, const void* q, const void* k, const void* v, const int32_t* cu_q,
+                             const int32_t* cu_k, const int32_t* len_q, const int32_t* len_k, const void* bias,
+                             const int32_t* buckets) {
+  vcja::PackedArgs a{};
+  a.q = bf(q);
+  a.k = bf(k);
+  a.v = bf(v);
+  a.cu_q = cu_q;
+  a.cu_k = cu_k;
+  a.len_q = len_q;
+  a.len_k = len_k;
+  if (d->num_buckets) {
+    a.bias = bf(bias);
+    a.buckets = buckets;
+    a.nb = d->num_buckets;
+    a.R = d->max_distance;
+  }
+  a.S = d->sequences;
+  a.H = d->heads;
+  a.Hkv = d->kv_heads;
+  a.G = d->heads / d->kv_heads;
+  a.Tq = (int)d->total_q;
+  a.Tk = (int)d->total_k;
+  a.max_q = d->max_q;
+  a.max_k = d->max_k;
+  a.q_tok = (unsigned)stride_of(d->q_stride, d->heads, d->head_dim);
+  a.k_tok = (unsigned)stride_of(d->k_stride, d->kv_heads, d->head_dim);
+  a.v_tok = (unsigned)stride_of(d->v_stride, d->kv_heads, d->head_dim);
+  a.causal = d->causal;
+  a.clear = d->clear_outside;
+  a.scale = scale_of(d);
+  a.scale_log2 = a.scale * vcja::kLog2e;
+  a.npad = (int)vcja::packed_rows(d->total_q, d->sequences);
+  return a;
+}
+
+// Backward workspace: -LSE/c | -D | the bias gradient's sums per distance.
+size_t stat_bytes(const vc_packedattn_desc* d) {
+  return align256((size_t)d->heads * vcja::packed_rows(d->total_q, d->sequences) * sizeof(float));
+}
+size_t dist_bytes(const vc_packedattn_desc* d) {
+  if (!d->num_buckets) return 0;
+  return align256((size_t)d->sequences * ((d->max_q + 255) / 256) * d->heads * (2 * d->max_distance + 1) * sizeof(float));
+}
+
+vc_status check_inputs(const vc_packedattn_desc* d, const void* q, const void* k, const void* v, const int32_t* cu_q,
+                       const int32_t* cu_k, const int32_t* len_q, const int32_t* len_k, const void* bias,
+                       const int32_t* buckets) {
+  if (!q || !k || !v || !cu_q || !cu_k || (d->num_buckets && (!bias || !buckets))) return VC_ERR_NULL;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned4(cu_q) || !aligned4(cu_k) || !aligned4(len_q) ||
+      !aligned4(len_k) || (d->num_buckets && ((reinterpret_cast<uintptr_t>(bias) & 1u) || !aligned4(buckets))))
+    return VC_ERR_ALIGN;
+  return VC_OK;
+}
+
+vc_status check_ws(const void* ws, size_t have, size_t need) {
+  if (!ws) return VC_ERR_WORKSPACE;
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return VC_ERR_ALIGN;
+  return have < need ? VC_ERR_WORKSPACE : VC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t vc_packedattn_fwd_workspace_bytes(const vc_packedattn_desc* desc) {
+  return check_packed(desc) == VC_OK ? 256 : 0;
+}
+
+vc_status vc_packedattn_fwd(const vc_packedattn_desc* desc, const void* q, const void* k, const void* v,
+                            const int32_t* cu_q, const int32_t* cu_k, const int32_t* len_q, const int32_t* len_k,
+                            const void* bias, const int32_t* buckets, void* o, float* lse, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  vc_status st = check_packed(desc);
+  if (st != VC_OK) return st;
+  if (!o || !lse) return VC_ERR_NULL;
+  if ((st = check_inputs(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets)) != VC_OK) return st;
+  if (!aligned16(o) || !aligned4(lse)) return VC_ERR_ALIGN;
+  if ((st = check_ws(workspace, workspace_bytes, vc_packedattn_fwd_workspace_bytes(desc))) != VC_OK) return st;
+  if ((st = vcja::check_device()) != VC_OK) return st;
+  vcja::PackedArgs a = packed_args(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets);
+  a.o = static_cast<__bf16*>(o);
+  a.lse = lse;
+  return vcja::launch_packed_fwd(a, desc->head_dim, as_stream(stream)) == hipSuccess ? VC_OK : VC_ERR_HIP;
+}
+
+size_t vc_packedattn_bwd_workspace_bytes(const vc_packedattn_desc* desc) {
+  return check_packed(desc) == VC_OK ? 2 * stat_bytes(desc) + dist_bytes(desc) : 0;
+}
+
+vc_status vc_packedattn_bwd(const vc_packedattn_desc* desc, const void* q, const void* k, const void* v, const void* o,
+                            const float* lse, const void* dout, const int32_t* cu_q, const int32_t* cu_k,
+                            const int32_t* len_q, const int32_t* len_k, const void* bias, const int32_t* buckets, void* dq,
+                            void* dk, void* dv, void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
+  vc_status st = check_packed(desc);
+  if (st != VC_OK) return st;
+  if (!o || !lse || !dout || !dq || !dk || !dv) return VC_ERR_NULL;
+  if ((st = check_inputs(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets)) != VC_OK) return st;
+  if (!aligned16(o) || !aligned4(lse) || !aligned16(dout) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) ||
+      (reinterpret_cast<uintptr_t>(dbias) & 1u))
+    return VC_ERR_ALIGN;
+  if (dbias && !desc->num_buckets) return VC_ERR_SHAPE;
+  if ((st = check_ws(workspace, workspace_bytes, vc_packedattn_bwd_workspace_bytes(desc))) != VC_OK) return st;
+  if ((st = vcja::check_device()) != VC_OK) return st;
+  vcja::PackedArgs a = packed_args(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets);
+  a.o_in = bf(o);
+  a.lse = const_cast<float*>(lse);
+  a.dout = bf(dout);
+  a.dq = static_cast<__bf16*>(dq);
+  a.dk = static_cast<__bf16*>(dk);
+  a.dv = static_cast<__bf16*>(dv);
+  char* ws = static_cast<char*>(workspace);
+  a.nls = reinterpret_cast<float*>(ws);
+  a.dd = reinterpret_cast<float*>(ws + stat_bytes(desc));
+  a.dist_part = reinterpret_cast<float*>(ws + 2 * stat_bytes(desc));
+  return vcja::launch_packed_bwd(a, desc->head_dim, static_cast<__bf16*>(dbias), as_stream(stream)) == hipSuccess ? VC_OK
+                                                                                                            : VC_ERR_HIP;
+}
+
+}  // extern "C"
+
+namespace {
+
+vc_status check_norm(const vc_layernorm_desc* d) {
+  if (!d) return VC_ERR_NULL;
+  if (d->rows < 1 || d->rows > kMaxRows || d->cols < 1 || d->cols > (1 << 16)) return VC_ERR_SHAPE;
+  for (const int t : {d->x_type, d->param_type})
+    if (t != VC_BF16 && t != VC_FP32) return VC_ERR_UNSUPPORTED;
+  for (const int64_t s : {d->x_stride, d->dout_stride})
+    if (s && (s < d->cols || s > ((int64_t)1 << 30))) return VC_ERR_SHAPE;
+  if (!(d->eps >= 0.0f && isfinite(d->eps))) return VC_ERR_SHAPE;
+  return VC_OK;
+}
+bool aligned_elem(const void* p, int type) { return (reinterpret_cast<uintptr_t>(p) & (type == VC_BF16 ? 1u : 3u)) == 0; }
+
+vcja::NormArgs norm_args(const vc_layernorm_desc* d, const void* x, const void* weight) {
+  vcja::NormArgs a{};
+  a.x = x;
+  a.w = weight;
+  a.rows = (int)d->rows;
+  a.cols = d->cols;
+  a.stride = d->x_stride ? d->x_stride : d->cols;
+  a.dout_stride = d->dout_stride ? d->dout_stride : d->cols;
+  a.eps = d->eps;
+  a.x_f32 = d->x_type == VC_FP32;
+  a.p_f32 = d->param_type == VC_FP32;
+  a.groups = vcja::norm_groups(d->rows, d->cols);
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+vc_status vc_layernorm_fwd(const vc_layernorm_desc* desc, const void* x, const void* weight, const void* bias, void* y,
+                           float* mean, float* rstd, void* stream) {
+  vc_status st = check_norm(desc);
+  if (st != VC_OK) return st;
+  if (!x || !y || !mean || !rstd) return VC_ERR_NULL;
+  if (!aligned_elem(x, desc->x_type) || !aligned_elem(y, desc->x_type) || !aligned_elem(weight, desc->param_type) ||
+      !aligned_elem(bias, desc->param_type) || !aligned4(mean) || !aligned4(rstd))
+    return VC_ERR_ALIGN;
+  if ((st = vcja::check_device()) != VC_OK) return st;
+  vcja::NormArgs a = norm_args(desc, x, weight);
+  a.b = bias;
+  a.y = y;
+  a.mean = mean;
+  a.rstd = rstd;
+  return vcja::launch_norm_fwd(a, as_stream(stream)) == hipSuccess ? VC_OK : VC_ERR_HIP;
+}
+
+size_t vc_layernorm_bwd_workspace_bytes(const vc_layernorm_desc* desc) {
+  if (check_norm(desc) != VC_OK) return 0;
+  return align256((size_t)2 * vcja::norm_groups(desc->rows, desc->cols) * desc->cols * sizeof(float));
+}
+
+vc_status vc_layernorm_bwd(const vc_layernorm_desc* desc, const void* dout, const void* x, const void* weight,
+                           const float* mean, const float* rstd, void* dx, void* dweight, void* dbias, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  vc_status st = check_norm(desc);
+  if (st != VC_OK) return st;
+  if (!dout || !x || !mean || !rstd || !dx) return VC_ERR_NULL;
+  if (!aligned_elem(dout, desc->x_type) || !aligned_elem(x, desc->x_type) || !aligned_elem(dx, desc->x_type) ||
+      !aligned_elem(weight, desc->param_type) || !aligned_elem(dweight, desc->param_type) ||
+      !aligned_elem(dbias, desc->param_type) || !aligned4(mean) || !aligned4(rstd))
+    return VC_ERR_ALIGN;
+  if ((dweight || dbias) && (st = check_ws(workspace, workspace_bytes, vc_layernorm_bwd_workspace_bytes(desc))) != VC_OK)
+    return st;
+  if ((st = vcja::check_device()) != VC_OK) return st;
+  vcja::NormArgs a = norm_args(desc, x, weight);
+  a.dout = dout;
+  a.mean = const_cast<float*>(mean);
+  a.rstd = const_cast<float*>(rstd);
+  a.dx = dx;
+  a.dw = dweight;
+  a.db = dbias;
+  a.part = static_cast<float*>(workspace);
+  return vcja::launch_norm_bwd(a, as_stream(stream)) == hipSuccess ? VC_OK : VC_ERR_HIP;
+}
+
+}  // extern "C"

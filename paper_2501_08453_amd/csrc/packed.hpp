@@ -1,0 +1,106 @@
+// Device-side types and helpers shared by the packed-attention kernels (gfx950).
+#pragma once
+
+#include "common.hpp"
+
+namespace vcja {
+
+constexpr int kMaxBiasDistance = 512;  // largest relative distance with a bucket of its own
+constexpr int kMaxBuckets = 1024;
+constexpr float kBiasLimit = 65536.0f;  // bias entries below -this shut their pairs out
+
+// Kernel arguments of the packed attention. Sequence s has the query slot [cu_q[s], cu_q[s+1])
+// of the Tq rows and the key slot [cu_k[s], cu_k[s+1]) of the Tk rows; the first len_q[s] and
+// len_k[s] rows of them (all without the arrays) take part.
+struct PackedArgs {
+  const __bf16 *q, *k, *v;
+  const __bf16* dout;  // backward
+  const __bf16* o_in;  // backward: the forward's O
+  __bf16 *o, *dq, *dk, *dv;
+  float* lse;          // [H, Tq]; the backward reads it
+  const int32_t *cu_q, *cu_k, *len_q, *len_k;
+  const __bf16* bias;      // [H, nb] or NULL
+  const int32_t* buckets;  // [2 R + 1], of the distances -R .. R
+  int nb, R;
+  int S, H, Hkv, G;        // G = H / Hkv query heads per key head
+  int Tq, Tk, max_q, max_k;
+  unsigned q_tok, k_tok, v_tok;  // elements between the rows of consecutive tokens
+  int causal, clear;
+  float scale, scale_log2;  // softmax scale; times log2(e)
+  int nblk;                 // row blocks of the longest slot
+  // Backward: per query row -LSE / c (-inf on padding) and -D, [H, npad], sequence s from row
+  // packed_row(cu_q[s], s) on.
+  float *nls, *dd;
+  int npad;
+  float* dist_part;         // bias gradient: per (sequence, row block, head) the sums per distance
+};
+
+// The rows of one sequence. Whatever the offsets hold, they stay inside the tensors.
+struct SeqRows {
+  int q0, sq, nq;  // first row, rows of the slot, rows that take part
+  int k0, sk, nk;
+  int off;         // query i stands at position i + off of the keys: the last at the last key
+};
+__device__ __forceinline__ SeqRows seq_rows(const PackedArgs& a, int s) {
+  SeqRows r;
+  r.q0 = min(max(a.cu_q[s], 0), a.Tq);
+  r.sq = min(max(a.cu_q[s + 1], r.q0), a.Tq) - r.q0;
+  r.sq = min(r.sq, a.max_q);
+  r.nq = a.len_q ? min(max(a.len_q[s], 0), r.sq) : r.sq;
+  r.k0 = min(max(a.cu_k[s], 0), a.Tk);
+  r.sk = min(max(a.cu_k[s + 1], r.k0), a.Tk) - r.k0;
+  r.sk = min(r.sk, a.max_k);
+  r.nk = a.len_k ? min(max(a.len_k[s], 0), r.sk) : r.sk;
+  r.off = r.nk - r.nq;
+  return r;
+}
+// Row of query i; past the sequence's own rows its last one (never another's: those may hold
+// anything), and some row of the tensor where there is none.
+__device__ __forceinline__ int query_row(const PackedArgs& a, const SeqRows& r, int i) {
+  return min(r.q0 + max(min(i, r.nq - 1), 0), a.Tq - 1);
+}
+// First row of sequence s in the padded row statistics: a multiple of 64, at least the
+// sequence's rows rounded up to 64 before the next one's.
+__host__ __device__ constexpr int packed_row(int q0, int s) { return ((q0 + 63) & ~63) + 64 * s; }
+__host__ __device__ constexpr int64_t packed_rows(int64_t Tq, int64_t S) { return ((Tq + 63) & ~(int64_t)63) + 64 * (S + 1) + 256; }
+
+// Sums and offsets of one (row block, head, sequence) item of a 1-D grid: heads and sequences
+// run fastest, key heads before the query heads of a group, so that (with 8 key heads or a
+// multiple) the workgroups that read a key head's rows sit on one XCD; the last row blocks, the
+// longest under the causal rule, are dispatched first.
+struct PackedItem {
+  int blk, h, s;
+};
+__device__ __forceinline__ PackedItem packed_item(int x, int nblk, int Hkv, int G, int S) {
+  const int HS = Hkv * G * S, p = x % HS, hx = p % (Hkv * G);
+  return PackedItem{nblk - 1 - x / HS, (hx % Hkv) * G + hx / Hkv, p / (Hkv * G)};
+}
+
+// Bias of one head per distance in LDS, divided by the softmax scale (the scores' own unit):
+// entry kBiasPad + R + d for distance d = key position - query position, distances past +-R
+// repeating the last, so that no tile that holds a distance inside (-R, R) reads outside.
+constexpr int kBiasPad = 96;  // >= 63 + 31, the distances in a tile of 64 keys x 32 queries
+constexpr int kBiasTable = 2 * kMaxBiasDistance + 1 + 2 * kBiasPad;
+__device__ __forceinline__ void load_bias_table(const PackedArgs& a, int h, float* tb, int tid, int threads) {
+  const float inv = 1.0f / a.scale;
+  for (int i = tid; i < 2 * a.R + 1 + 2 * kBiasPad; i += threads) {
+    const int u = a.buckets[min(max(i - kBiasPad, 0), 2 * a.R)];
+    float b = u >= 0 && u < a.nb ? (float)a.bias[(size_t)h * a.nb + u] : 0.0f;
+    b = b < -kBiasLimit ? -INFINITY : b > kBiasLimit ? kBiasLimit : b;  // a NaN stays one
+    tb[i] = b * inv;
+  }
+}
+
+// Where a block of keys [k0, k1] stands to a block of query positions [p0, p1]: every distance
+// at or past R (1), at or before -R (-1), or some inside (0).
+__device__ __forceinline__ int bias_side(int k0, int k1, int p0, int p1, int R) {
+  return k0 - p1 >= R ? 1 : k1 - p0 <= -R ? -1 : 0;
+}
+
+}  // namespace vcja
+
+// Host-side launchers.
+namespace vcja {
+hipError_t launch_packed_fwd(const PackedArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_packed_bwd(const PackedArgs& a, int head_dim, __bf16* dbias, hipStream_t s);
+}  // namespace vcja

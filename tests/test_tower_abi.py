@@ -1,0 +1,154 @@
+"""Refusals of the packed attention's and the layer norm's entry points (CPU: nothing here reaches a launch)."""
+import ctypes
+
+import pytest
+
+import paper_2501_08453_amd as vc
+
+P = 1 << 20  # never dereferenced: validation fails first
+BIG = 1 << 40
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return vc._lib()
+
+
+def desc(**kw):
+    d = vc.make_packed_desc(3, 4, 2, 64, 100, 120, 60, 70)
+    for n, x in kw.items():
+        setattr(d, n, x)
+    return d
+
+
+def fwd(lib, d, q=P, k=P, v=P, cu_q=P, cu_k=P, len_q=None, len_k=None, bias=None, buckets=None, o=P, lse=P, ws=P, n=BIG):
+    return lib.vc_packedattn_fwd(d and ctypes.byref(d), q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets, o, lse, ws, n, None)
+
+
+def bwd(lib, d, q=P, k=P, v=P, o=P, lse=P, dout=P, cu_q=P, cu_k=P, len_q=None, len_k=None, bias=None, buckets=None, dq=P, dk=P, dv=P,
+        dbias=None, ws=P, n=BIG):
+    return lib.vc_packedattn_bwd(d and ctypes.byref(d), q, k, v, o, lse, dout, cu_q, cu_k, len_q, len_k, bias, buckets, dq, dk, dv,
+                                 dbias, ws, n, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(head_dim=96), -3), (dict(head_dim=0), -3), (dict(sequences=0), -2), (dict(heads=0), -2), (dict(kv_heads=0), -2),
+    (dict(kv_heads=3), -2), (dict(heads=8192, kv_heads=2), -2), (dict(total_q=0), -2), (dict(total_k=0), -2),
+    (dict(total_q=1 << 31), -2), (dict(max_q=0), -2), (dict(max_q=101), -2), (dict(max_k=121), -2), (dict(causal=2), -2),
+    (dict(clear_outside=-1), -2), (dict(q_stride=255), -2), (dict(q_stride=4 * 64 + 4), -2), (dict(k_stride=120), -2),
+    (dict(v_stride=-128), -2), (dict(q_stride=1 << 24), -2), (dict(num_buckets=-1), -2), (dict(num_buckets=1025), -2),
+    (dict(num_buckets=4, max_distance=513), -2), (dict(max_distance=-1), -2), (dict(softmax_scale=float("nan")), -2),
+    (dict(softmax_scale=float("inf")), -2), (dict(softmax_scale=2.0 ** -61), -2),
+    (dict(softmax_scale=2.0 ** -25, num_buckets=4), -2), (dict(softmax_scale=2.0 ** 25, num_buckets=4), -2),
+    (dict(sequences=1 << 20, heads=4096, total_q=1 << 29, total_k=1 << 29, max_q=1 << 20, max_k=1), -2),
+])
+def test_bad_descriptor(lib, kw, code):
+    d = desc(**kw)
+    assert fwd(lib, d, bias=P, buckets=P) == code
+    assert bwd(lib, d, bias=P, buckets=P) == code
+    assert vc.vc_packedattn_fwd_workspace_bytes(d) == 0 and vc.vc_packedattn_bwd_workspace_bytes(d) == 0
+
+
+def test_pointers_and_workspaces(lib):
+    d, b = desc(), desc(num_buckets=4, max_distance=3)
+    assert fwd(lib, None) == -1 and bwd(lib, None) == -1
+    for n in ("q", "k", "v", "cu_q", "cu_k", "o", "lse"):
+        assert fwd(lib, d, **{n: None}) == -1, n
+        assert fwd(lib, d, **{n: P + 2}) == -4, n
+    for n in ("q", "k", "v", "o", "lse", "dout", "cu_q", "cu_k", "dq", "dk", "dv"):
+        assert bwd(lib, d, **{n: None}) == -1, n
+        assert bwd(lib, d, **{n: P + 2}) == -4, n
+    for n in ("len_q", "len_k"):
+        assert fwd(lib, d, **{n: P + 2}) == -4 and bwd(lib, d, **{n: P + 2}) == -4
+    assert fwd(lib, b, bias=P) == -1 and fwd(lib, b, buckets=P) == -1 and bwd(lib, b, bias=P) == -1
+    assert fwd(lib, b, bias=P + 1, buckets=P) == -4 and fwd(lib, b, bias=P, buckets=P + 2) == -4
+    assert bwd(lib, d, dbias=P) == -2  # a gradient of a bias that is not there
+    for f, need in ((fwd, vc.vc_packedattn_fwd_workspace_bytes(d)), (bwd, vc.vc_packedattn_bwd_workspace_bytes(d))):
+        assert need > 0
+        assert f(lib, d, ws=None) == -5 and f(lib, d, n=need - 1) == -5 and f(lib, d, ws=P + 16) == -4
+    import torch
+    if not torch.cuda.is_available():
+        assert fwd(lib, d) == -6 and bwd(lib, b, bias=P, buckets=P, dbias=P) == -6
+
+
+def test_norm_refusals(lib):
+    def norm(**kw):
+        d = vc.vc_layernorm_desc(10, 100, 0, 1, 1e-5, 0, 0)
+        for n, x in kw.items():
+            setattr(d, n, x)
+        return d
+
+    def f(d, x=P, w=P, b=P, y=P, m=P, r=P):
+        return lib.vc_layernorm_fwd(d and ctypes.byref(d), x, w, b, y, m, r, None)
+
+    def g(d, dy=P, x=P, w=P, m=P, r=P, dx=P, dw=P, db=P, ws=P, n=BIG):
+        return lib.vc_layernorm_bwd(d and ctypes.byref(d), dy, x, w, m, r, dx, dw, db, ws, n, None)
+
+    for kw, code in ((dict(rows=0), -2), (dict(rows=1 << 31), -2), (dict(cols=0), -2), (dict(cols=65537), -2), (dict(x_type=2), -8),
+                     (dict(param_type=-1), -8), (dict(x_stride=99), -2), (dict(dout_stride=-1), -2), (dict(eps=-1.0), -2),
+                     (dict(eps=float("nan")), -2)):
+        assert f(norm(**kw)) == code and g(norm(**kw)) == code, kw
+        assert vc.vc_layernorm_bwd_workspace_bytes(norm(**kw)) == 0
+    assert f(None) == -1 and g(None) == -1
+    for n in "xymr":
+        assert f(norm(), **{n: None}) == -1 and f(norm(), **{n: P + 1}) == -4
+    for n in ("dy", "x", "m", "r", "dx"):
+        assert g(norm(), **{n: None}) == -1 and g(norm(), **{n: P + 1}) == -4
+    assert f(norm(), w=P + 2) == -4 and f(norm(x_type=1), x=P + 2) == -4 and g(norm(), dw=P + 2) == -4
+    need = vc.vc_layernorm_bwd_workspace_bytes(norm())
+    assert need > 0 and g(norm(), ws=None) == -5 and g(norm(), n=need - 1) == -5 and g(norm(), ws=P + 16) == -4
+    import torch
+    if not torch.cuda.is_available():
+        assert f(norm(), w=None, b=None) == -6 and g(norm(), dw=None, db=None, ws=None, n=0) == -6
+
+
+def test_helpers_check_before_calling():
+    torch = pytest.importorskip("torch")
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)  # noqa: E731
+    q, k, v = bf(100, 4, 64), bf(120, 2, 64), bf(120, 2, 64)
+    cu = torch.zeros(4, dtype=torch.int32)
+    d = vc.make_packed_desc(3, 4, 2, 64, 100, 120, 60, 70)
+    b = vc.make_packed_desc(3, 4, 2, 64, 100, 120, 60, 70, num_buckets=5, max_distance=2)
+    bias, buckets = bf(4, 5), torch.zeros(5, dtype=torch.int32)
+    for match, call in (
+            ("must be on a GPU", lambda: vc.packed_fwd(q, k, v, d, cu, cu)),
+            ("q has shape", lambda: vc.packed_fwd(q[:-1], k, v, d, cu, cu)),
+            ("k must be torch.bfloat16", lambda: vc.packed_fwd(q, k.float(), v, d, cu, cu)),
+            ("v has shape", lambda: vc.packed_fwd(q, k, bf(120, 4, 64), d, cu, cu)),
+            ("cu_q must be torch.int32", lambda: vc.packed_fwd(q, k, v, d, cu.long(), cu)),
+            ("cu_k has shape", lambda: vc.packed_fwd(q, k, v, d, cu, cu[:-1])),
+            ("len_k has shape", lambda: vc.packed_fwd(q, k, v, d, cu, cu, len_k=cu)),
+            ("a bias and its buckets", lambda: vc.packed_fwd(q, k, v, d, cu, cu, bias=bias, buckets=buckets)),
+            ("a bias and its buckets", lambda: vc.packed_fwd(q, k, v, b, cu, cu)),
+            ("a bias and its buckets", lambda: vc.packed_fwd(q, k, v, b, cu, cu, bias=bias)),
+            ("bias must be torch.bfloat16", lambda: vc.packed_fwd(q, k, v, b, cu, cu, bias=bias.float(), buckets=buckets)),
+            ("buckets has shape", lambda: vc.packed_fwd(q, k, v, b, cu, cu, bias=bias, buckets=buckets[:-1])),
+            ("out has shape", lambda: vc.packed_fwd(q, k, v, d, cu, cu, out=k)),
+            ("lse has shape", lambda: vc.packed_fwd(q, k, v, d, cu, cu, lse=torch.zeros(100, 4))),
+            ("given together", lambda: vc.packed_bwd(q, k, v, q, torch.zeros(4, 100), q, d, cu, cu, dq=q)),
+            ("dout must be", lambda: vc.packed_bwd(q, k, v, q, torch.zeros(4, 100), q.float(), d, cu, cu)),
+            ("invalid descriptor", lambda: vc.packed_fwd_workspace(vc.make_packed_desc(3, 4, 3, 64, 9, 9, 9, 9), "cpu")),
+            ("relative_buckets", lambda: vc.relative_buckets(2, 8)),
+            ("relative_buckets", lambda: vc.relative_buckets(32, 8)),
+            ("relative_buckets", lambda: vc.relative_buckets(32, 513)),
+            ("x must be torch", lambda: vc.layer_norm_fwd(q.half())),
+            ("x must be on a GPU", lambda: vc.layer_norm_fwd(q)),
+            ("weight has shape", lambda: vc.layer_norm_fwd(q, bf(63))),
+            ("weight and bias", lambda: vc.layer_norm_fwd(q, bf(64), torch.zeros(64))),
+            ("rstd has shape", lambda: vc.layer_norm_bwd(q, q, None, None, torch.zeros(100, 4), torch.zeros(100))),
+    ):
+        with pytest.raises(ValueError, match=match):
+            call()
+
+
+def test_relative_buckets():
+    """The borders hold in whole numbers: with 8 buckets a direction, 4 wide ones up to 64 = 4 * 16, distance 8 = 4 * 16^(1/4)
+    * ... is the first of its bucket where 8^4 >= 64 * 4^3."""
+    b = vc.relative_buckets(16, 64, device="cpu").tolist()
+    assert len(b) == 129 and b[64] == 0 and b[63] == 1 and b[65] == 9
+    behind = b[64::-1]  # n = 0 .. 64
+    assert behind[:4] == [0, 1, 2, 3] and behind[7] == 4 and behind[8] == 5 and behind[15] == 5 and behind[16] == 6
+    assert behind[31] == 6 and behind[32] == 7 and behind[64] == 7
+    assert b[65:] == [8 + x for x in behind[1:]]
+    one = vc.relative_buckets(8, 64, bidirectional=False, device="cpu").tolist()
+    assert one[64::-1] == behind and one[65:] == [0] * 64
