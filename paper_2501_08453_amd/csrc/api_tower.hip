@@ -93,9 +93,24 @@ vcja::PackedArgs packed_args(const vc_packedattn_desc* d, const void* q, const v
 size_t stat_bytes(const vc_packedattn_desc* d) {
   return align256((size_t)d->heads * vcja::packed_rows(d->total_q, d->sequences) * sizeof(float));
 }
+// Backward: workgroups of four waves (128 rows) or eight, and the chunks of a key block's query tiles.
+bool small_blocks(const vc_packedattn_desc* d) { return std::max(d->max_q, d->max_k) <= 2048; }
+int key_chunks(const vc_packedattn_desc* d) {
+  if (d->num_buckets) return d->heads / d->kv_heads;
+  const int bm = small_blocks(d) ? 128 : 256, group = d->heads / d->kv_heads;
+  const int64_t blocks = std::min<int64_t>((int64_t)d->sequences * ((d->max_k + bm - 1) / bm), d->total_k / bm + d->sequences);
+  const int64_t want = (1024 + d->kv_heads * blocks - 1) / (d->kv_heads * blocks);
+  const int64_t steps = (int64_t)group * ((d->max_q + 31) / 32);
+  return (int)std::max<int64_t>(1, std::min(want, steps / 8));
+}
 size_t dist_bytes(const vc_packedattn_desc* d) {
   if (!d->num_buckets) return 0;
-  return align256((size_t)d->sequences * ((d->max_q + 255) / 256) * d->heads * (2 * d->max_distance + 1) * sizeof(float));
+  const int bm = small_blocks(d) ? 128 : 256;
+  return align256((size_t)d->sequences * ((d->max_k + bm - 1) / bm) * d->heads * (2 * d->max_distance + 1) * sizeof(float));
+}
+size_t key_part_bytes(const vc_packedattn_desc* d) {
+  const int c = key_chunks(d);
+  return c == 1 ? 0 : align256((size_t)c * 2 * d->total_k * d->kv_heads * d->head_dim * sizeof(float));
 }
 
 vc_status check_inputs(const vc_packedattn_desc* d, const void* q, const void* k, const void* v, const int32_t* cu_q,
@@ -140,7 +155,7 @@ vc_status vc_packedattn_fwd(const vc_packedattn_desc* desc, const void* q, const
 }
 
 size_t vc_packedattn_bwd_workspace_bytes(const vc_packedattn_desc* desc) {
-  return check_packed(desc) == VC_OK ? 2 * stat_bytes(desc) + dist_bytes(desc) : 0;
+  return check_packed(desc) == VC_OK ? 2 * stat_bytes(desc) + dist_bytes(desc) + key_part_bytes(desc) : 0;
 }
 
 vc_status vc_packedattn_bwd(const vc_packedattn_desc* desc, const void* q, const void* k, const void* v, const void* o,
@@ -168,6 +183,9 @@ vc_status vc_packedattn_bwd(const vc_packedattn_desc* desc, const void* q, const
   a.nls = reinterpret_cast<float*>(ws);
   a.dd = reinterpret_cast<float*>(ws + stat_bytes(desc));
   a.dist_part = reinterpret_cast<float*>(ws + 2 * stat_bytes(desc));
+  a.key_part = reinterpret_cast<float*>(ws + 2 * stat_bytes(desc) + dist_bytes(desc));
+  a.small = small_blocks(desc);
+  a.chunks = key_chunks(desc);
   return vcja::launch_packed_bwd(a, desc->head_dim, static_cast<__bf16*>(dbias), as_stream(stream)) == hipSuccess ? VC_OK
                                                                                                             : VC_ERR_HIP;
 }

@@ -27,7 +27,10 @@ struct PackedArgs {
   unsigned q_tok, k_tok, v_tok;  // elements between the rows of consecutive tokens
   int causal, clear;
   float scale, scale_log2;  // softmax scale; times log2(e)
-  int nblk;                 // row blocks of the longest slot
+  int nblk, bm;             // row blocks of the longest slot, rows of one
+  bool small;               // workgroups of four waves instead of eight
+  int chunks;               // backward: workgroups that share a key block's query tiles
+  float* key_part;          // their partial dK, dV: [chunks][2][Tk, Hkv, D]
   // Backward: per query row -LSE / c (-inf on padding) and -D, [H, npad], sequence s from row
   // packed_row(cu_q[s], s) on.
   float *nls, *dd;
@@ -35,22 +38,35 @@ struct PackedArgs {
   float* dist_part;         // bias gradient: per (sequence, row block, head) the sums per distance
 };
 
+// A pointer that is the same for the whole wave, in scalar registers.
+template <class T>
+__device__ __forceinline__ T* uniform_ptr(T* p) {
+  const uint64_t x = (uint64_t)p;
+  const uint64_t lo = (unsigned)__builtin_amdgcn_readfirstlane((unsigned)x), hi = (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(x >> 32));
+  return (T*)(lo | hi << 32);
+}
+
+__device__ __forceinline__ float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
+
 // The rows of one sequence. Whatever the offsets hold, they stay inside the tensors.
 struct SeqRows {
   int q0, sq, nq;  // first row, rows of the slot, rows that take part
   int k0, sk, nk;
   int off;         // query i stands at position i + off of the keys: the last at the last key
 };
+// (`s` the same for the whole wave.)
 __device__ __forceinline__ SeqRows seq_rows(const PackedArgs& a, int s) {
+  // the same for the whole wave: in scalar registers
+  auto at = [&](const int32_t* p, int i) { return __builtin_amdgcn_readfirstlane(p[i]); };
   SeqRows r;
-  r.q0 = min(max(a.cu_q[s], 0), a.Tq);
-  r.sq = min(max(a.cu_q[s + 1], r.q0), a.Tq) - r.q0;
+  r.q0 = min(max(at(a.cu_q, s), 0), a.Tq);
+  r.sq = min(max(at(a.cu_q, s + 1), r.q0), a.Tq) - r.q0;
   r.sq = min(r.sq, a.max_q);
-  r.nq = a.len_q ? min(max(a.len_q[s], 0), r.sq) : r.sq;
-  r.k0 = min(max(a.cu_k[s], 0), a.Tk);
-  r.sk = min(max(a.cu_k[s + 1], r.k0), a.Tk) - r.k0;
+  r.nq = a.len_q ? min(max(at(a.len_q, s), 0), r.sq) : r.sq;
+  r.k0 = min(max(at(a.cu_k, s), 0), a.Tk);
+  r.sk = min(max(at(a.cu_k, s + 1), r.k0), a.Tk) - r.k0;
   r.sk = min(r.sk, a.max_k);
-  r.nk = a.len_k ? min(max(a.len_k[s], 0), r.sk) : r.sk;
+  r.nk = a.len_k ? min(max(at(a.len_k, s), 0), r.sk) : r.sk;
   r.off = r.nk - r.nq;
   return r;
 }

@@ -2,21 +2,22 @@
 //
 // dQ (query-stationary, first): one workgroup of eight waves owns 256 query rows of one
 //   (sequence, head), each wave 32, with Q^T and dO^T of its queries in registers. It forms
-//   D_i = <dO_i, O_i> from its own rows and writes -D and -LSE / c for the other pass, walks
-//   over the key tiles like the forward, computing S^T, dP^T and dS^T = P^T o (dP^T - D), and
-//   dQ^T += K^T dS^T.
-//   With a bias it also sums dS over every distance (see distance_sums).
+//   D_i = <dO_i, O_i> from its own rows and walks over the key tiles like the forward, computing
+//   S^T, dP^T and dS^T = P^T o (dP^T - D), and dQ^T += K^T dS^T. It leaves -LSE / c and -D for the
+//   other pass.
 // dK/dV (key-stationary): one workgroup owns 256 keys of one (sequence, key head), each wave 32,
 //   K and V of its keys in registers, and walks over the query tiles of 32 of every query head
-//   of the group, so that dK and dV of the shared head are summed in registers.
+//   of the group, so that dK and dV of the shared head are summed in registers; where that leaves
+//   too few workgroups, each takes a run of those tiles and fp32 partials are summed afterwards.
+//   With a bias it also sums dS over every distance (see distance_sums).
 // No atomics anywhere: results are bitwise reproducible.
+#include <type_traits>
+
 #include "packed.hpp"
 
 namespace vcja {
 namespace {
 
-constexpr int kWaves = 8;
-constexpr int kBM = 32 * kWaves;   // queries (keys) per workgroup
 constexpr int kBN = kTileTok;      // keys per dQ tile
 constexpr int kBQ = 32;            // queries per dK/dV tile
 
@@ -27,20 +28,21 @@ __device__ __forceinline__ bf16x8 operand(const f32x16& x, int half) {
   return y;
 }
 
-// Sums of one 32 keys x 32 queries block of dS^T over its diagonals (distance = key - query),
-// without atomics. Register r of lane (col t, half hi) holds key row kr = 8 (r / 4) + 4 hi + r % 4:
-// rotating it by kr brings distance t (where kr >= t) or t - 32 to lane t, the same for every
-// register, so that a lane adds its own values up; the two halves of the wave are joined at
-// the end, the lower one keeping distances 0 .. 31, the upper one -32 .. -1.
+// Sums of one 32 queries x 32 keys block of dS over its diagonals (distance = key - query), without
+// atomics. Register r of a lane of half hi holds query row n = 8 (r / 4) + 4 hi + r % 4 of its
+// key: rotating it by n brings distance t (where n + t < 32) or t - 32 to lane t, the same for
+// every register, so that a lane adds its own values up; the two halves of the wave are joined
+// at the end, the lower one keeping distances 0 .. 31, the upper one -32 .. -1.
 __device__ __forceinline__ float distance_sums(const f32x16& ds, int lane) {
   const int t = lane & 31, hi = lane >> 5;
   float pos = 0.0f, neg = 0.0f;
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
-    const int kr = acc_row(r, hi);
-    const float x = __shfl(ds[r], (lane & 32) | ((kr - t) & 31), 64);
-    pos += t <= kr ? x : 0.0f;
-    neg += t <= kr ? 0.0f : x;
+    if (r % 4 == 0) sched_fence();  // a few at a time: registers are the limit here
+    const int n = acc_row(r, hi);
+    const float x = __shfl(ds[r], (lane & 32) | ((n + t) & 31), 64);
+    pos += n + t < 32 ? x : 0.0f;
+    neg += n + t < 32 ? 0.0f : x;
   }
   pos = halves_sum(pos);
   neg = halves_sum(neg);
@@ -53,46 +55,72 @@ __device__ __forceinline__ float wave_sum(float x) {
   return x;
 }
 
-template <int D, bool BIAS>
-__global__ __launch_bounds__(64 * kWaves, 1) void packed_dq_kernel(PackedArgs a) {
+// Rows outside every slot of a tensor's [rows, H, D]: zero (the last workgroups of a grid).
+template <int D>
+__device__ __forceinline__ void clear_rows(__bf16* x, __bf16* y, const int32_t* cu, int S, int total, int H, int wg, int wgs, int tid,
+                                           int threads) {
+  const int head = min(max(cu[0], 0), total), end = min(max(cu[S], head), total);
+  const int64_t per = (int64_t)H * (D / 8);
+  for (int64_t i = (int64_t)wg * threads + tid; i < (head + total - end) * per; i += (int64_t)wgs * threads) {
+    const int r = (int)(i / per);
+    const size_t at = (size_t)(r < head ? r : r - head + end) * H * D + i % per * 8;
+    *(bf16x8*)(x + at) = zero_bf16x8();
+    if (y) *(bf16x8*)(y + at) = zero_bf16x8();
+  }
+}
+
+template <int D, int NW, bool BIAS>
+__global__ __launch_bounds__(64 * NW, 8 / NW) void packed_dq_kernel(PackedArgs a) {
   using Rows = SwzRows<D>;
   using Reads = SwzReads<D>;
+  constexpr int BM = 32 * NW;
   constexpr int RT = Rows::bytes(kBN);
-  constexpr int STAGE = 2 * RT;
-  constexpr int CPW = kBN / Rows::RPC / kWaves;
-  constexpr int HIST = 2 * kMaxBiasDistance + 1;
+  constexpr int STAGE = 2 * RT;                  // K | V rows of a tile
+  constexpr int CPW = kBN / Rows::RPC / NW;      // copies of each per wave
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
   __shared__ float tb[BIAS ? kBiasTable : 1];
-  __shared__ float hist[BIAS ? kWaves * HIST : 1];  // each wave's sums per distance
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hi = lane >> 5;
   const int items = a.nblk * a.H * a.S;
-  if ((int)blockIdx.x >= items) {  // rows outside every slot
-    const int wg = blockIdx.x - items, wgs = gridDim.x - items;
-    const int head = min(max(a.cu_q[0], 0), a.Tq), end = min(max(a.cu_q[a.S], head), a.Tq);
-    const int64_t per = (int64_t)a.H * (D / 8);
-    for (int64_t i = (int64_t)wg * blockDim.x + tid; i < (head + a.Tq - end) * per; i += (int64_t)wgs * blockDim.x) {
-      const int r = (int)(i / per);
-      *(bf16x8*)(a.dq + (size_t)(r < head ? r : r - head + end) * a.H * D + i % per * 8) = zero_bf16x8();
-    }
+  if ((int)blockIdx.x >= items) {
+    clear_rows<D>(a.dq, nullptr, a.cu_q, a.S, a.Tq, a.H, blockIdx.x - items, gridDim.x - items, tid, 64 * NW);
     return;
   }
   const PackedItem it = packed_item(blockIdx.x, a.nblk, a.Hkv, a.G, a.S);
   const SeqRows sr = seq_rows(a, it.s);
-  const int b0 = it.blk * kBM;
+  const int b0 = it.blk * BM;
   if (b0 >= sr.sq) return;
   const int kv = it.h / a.G;
   const int qi = b0 + w * 32 + l32;
   auto limit = [&](int i) { return a.causal ? max(0, min(sr.nk, i + sr.off + 1)) : sr.nk; };
-  const int qe = min(b0 + kBM, sr.nq);
+  const int qe = min(b0 + BM, sr.nq);
   const int blk_keys = qe > b0 ? limit(qe - 1) : 0;
   const int wave_keys = b0 + w * 32 < qe ? limit(min(b0 + w * 32 + 32, sr.nq) - 1) : 0;
   const int wave_all = limit(b0 + w * 32);
   const int klim = qi < sr.nq ? limit(qi) : 0;
   const int ntile = (blk_keys + kBN - 1) / kBN;
+
+  const SwzCopy<D, true> kc(a.k_tok, lane), vc(a.v_tok, lane);
+  const __bf16* kbase = a.k + (size_t)sr.k0 * a.k_tok + kv * D;
+  const __bf16* vbase = a.v + (size_t)sr.k0 * a.v_tok + kv * D;
+  auto issue_j = [&](int j, bool is_k, int kt, int st) {
+    const int idx = w + j * NW, first = swz_copy_row<D, true>(kt * kBN, sr.nk, idx);
+    VC_LDS char* dst = (VC_LDS char*)smem + st * STAGE + (is_k ? 0 : RT) + idx * Rows::GS;
+    if (is_k)
+      copy16_to_lds_opaque(kbase + (size_t)first * a.k_tok, kc.offset(first, sr.nk, a.k_tok), dst);
+    else
+      copy16_to_lds_opaque(vbase + (size_t)first * a.v_tok, vc.offset(first, sr.nk, a.v_tok), dst);
+  };
+  auto issue_tile = [&](int kt, int st) {
+#pragma unroll
+    for (int j = 0; j < CPW; ++j) {
+      issue_j(j, true, kt, st);
+      issue_j(j, false, kt, st);
+    }
+  };
 
   bf16x8 qf[D / 16], dof[D / 16];
   float nls, dd;
@@ -109,123 +137,146 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_dq_kernel(PackedArgs a)
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum = fmaf((float)o[e], (float)dof[ks][e], sum);
     }
-    dd = -halves_sum(sum);
+    dd = klim == 0 ? 0.0f : -halves_sum(sum);
     const float x = a.lse[(size_t)it.h * a.Tq + row];
     nls = klim == 0 || x == -INFINITY ? -INFINITY : -x / a.scale;
-    if (klim == 0) dd = 0.0f;
-    if (hi == 0 && qi < ((sr.nq + 63) & ~63)) {
-      const size_t p = (size_t)it.h * a.npad + packed_row(sr.q0, it.s) + qi;
-      a.nls[p] = nls;
-      a.dd[p] = dd;
-    }
   }
-  if (BIAS) {
-    load_bias_table(a, it.h, tb, tid, 64 * kWaves);
-    for (int i = tid; i < kWaves * HIST; i += 64 * kWaves) hist[i] = 0.0f;
-  }
-
-  const SwzCopy<D, true> kc(a.k_tok, lane), vc(a.v_tok, lane);
-  const __bf16* kbase = a.k + (size_t)sr.k0 * a.k_tok + kv * D;
-  const __bf16* vbase = a.v + (size_t)sr.k0 * a.v_tok + kv * D;
-  auto copy_tile = [&](int kt, int st) {
-#pragma unroll
-    for (int j = 0; j < CPW; ++j) {
-      const int idx = w + j * kWaves, first = swz_copy_row<D, true>(kt * kBN, sr.nk, idx);
-      VC_LDS char* dst = (VC_LDS char*)smem + st * STAGE + idx * Rows::GS;
-      copy16_to_lds_opaque(kbase + (size_t)first * a.k_tok, kc.offset(first, sr.nk, a.k_tok), dst);
-      copy16_to_lds_opaque(vbase + (size_t)first * a.v_tok, vc.offset(first, sr.nk, a.v_tok), dst + RT);
-    }
-  };
+  if (BIAS) load_bias_table(a, it.h, tb, tid, 64 * NW);
 
   f32x16 acc[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) acc[i] = zero_f32x16();
-  const int pos0 = b0 + w * 32 + sr.off;
+  const int pos0 = b0 + w * 32 + sr.off;  // position of the wave's first query
   const float nlse2 = nls * a.scale_log2;
-  float far_lo = 0.0f, far_hi = 0.0f;
+  float rowsum = 0.0f;
 
-  if (ntile > 0) copy_tile(0, 0);
+  if (ntile > 0) issue_tile(0, 0);
+  wait_all_memory();  // the loads above too: no later wait stands among copies
   for (int kt = 0; kt < ntile; ++kt) {
     const int st = kt & 1;
     wait_all_memory();
     __syncthreads();
-    if (kt + 1 < ntile) copy_tile(kt + 1, st ^ 1);
     const int k0 = kt * kBN;
-    if (k0 >= wave_keys) continue;
+    const int kn = min(kt + 1, ntile - 1);  // past the last tile: copied again, never read
+    if (k0 >= wave_keys) {
+      issue_tile(kn, st ^ 1);
+      continue;
+    }
+    // The two key blocks' products in one stretch of matrix-core ops, every LDS operand read
+    // PF ops ahead, the vector arithmetic of a phase placed between the ops of the next ones:
+    // S0 | dP0, P0 | S1, dS0 | dP1, P1 | dQ += K0^T dS0, dS1 | dQ += K1^T dS1.
+    constexpr int KSN = D / 16;
+    constexpr int NB = D / 32;
+    constexpr int PF = 3;
+    constexpr int EP = 16 / KSN;
     const VC_LDS char* tile = (const VC_LDS char*)smem + st * STAGE;
     const VC_LDS char* rp = tile + Reads::row_base(perm_row(l32), hi);
     const VC_LDS char* tp = tile + Reads::tr_base(lane);
+    bf16x8 f[4 * KSN], g[4 * NB];
+    auto rd = [&](int i) {  // S0, dP0, S1, dP1, then the dQ operands
+      if (i < 4 * KSN) {
+        const int kb = i / (2 * KSN), v = i / KSN % 2;
+        f[i] = *(const VC_LDS bf16x8*)(Reads::row_at(rp, i % KSN) + v * RT + kb * Rows::bytes(32));
+      } else if (i - 4 * KSN < 4 * NB) {
+        g[i - 4 * KSN] = Reads::tr_operand(tp, (i - 4 * KSN) / NB, (i - 4 * KSN) % NB);
+      }
+    };
+    f32x16 s[2], dp[2];
+    bf16x8 sb[4];
+    float shift[2] = {nlse2, nlse2};
+    auto form_p = [&](int kb, int r) { s[kb][r] = fast_exp2(fmaf(s[kb][r], a.scale_log2, shift[kb])); };
+    auto form_ds = [&](int kb, int r) {
+      dp[kb][r] *= s[kb][r];
+      rowsum += dp[kb][r];
+    };
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
-      f32x16 s = zero_f32x16(), dp;
-      int side = 0;
+      s[kb] = zero_f32x16();
       if (BIAS) {
-        side = bias_side(k0 + 32 * kb, k0 + 32 * kb + 31, pos0, pos0 + 31, a.R);
-        const float* t = tb + kBiasPad + a.R + (k0 + 32 * kb + 4 * hi - pos0 - l32);
-        const float c = tb[kBiasPad + (side > 0 ? 2 * a.R : 0)];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = c;
+        const int side = bias_side(k0 + 32 * kb, k0 + 32 * kb + 31, pos0, pos0 + 31, a.R);
         if (side == 0) {
+          const float* t = tb + kBiasPad + a.R + (k0 + 32 * kb + 4 * hi - pos0 - l32);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = t[8 * (r >> 2) + (r & 3)];
-        }
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) dp[r] = dd;
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        s = mfma32(*(const VC_LDS bf16x8*)(Reads::row_at(rp, ks) + kb * Rows::bytes(32)), qf[ks], s);
-        dp = mfma32(*(const VC_LDS bf16x8*)(Reads::row_at(rp, ks) + RT + kb * Rows::bytes(32)), dof[ks], dp);
-      }
-      if (k0 + 32 * kb + 32 > wave_all) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = k0 + 32 * kb + acc_row(r, hi) < klim ? s[r] : -INFINITY;
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) dp[r] *= fast_exp2(fmaf(s[r], a.scale_log2, nlse2));
-      if (BIAS) {
-        if (side == 0) {
-          const float x = distance_sums(dp, lane);
-          const int d = k0 + 32 * kb - pos0 + l32 - 32 * hi;
-          if (d <= -a.R)
-            far_lo += x;
-          else if (d >= a.R)
-            far_hi += x;
-          else
-            hist[w * HIST + d + a.R] += x;
+          for (int r = 0; r < 16; ++r) s[kb][r] = t[8 * (r >> 2) + (r & 3)];
         } else {
-          float x = 0.0f;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) x += dp[r];
-          far_lo += side < 0 ? x : 0.0f;
-          far_hi += side < 0 ? 0.0f : x;
+          shift[kb] = fmaf(tb[kBiasPad + (side > 0 ? 2 * a.R : 0)], a.scale_log2, nlse2);
         }
-      }
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const bf16x8 sb = operand(dp, half);
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db) acc[db] = mfma32(Reads::tr_operand(tp, 2 * kb + half, db), sb, acc[db]);
       }
     }
+#pragma unroll
+    for (int i = 0; i < PF; ++i) rd(i);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int i = 0; i < KSN; ++i) {
+        sched_fence();
+        rd(2 * KSN * kb + i + PF);
+        s[kb] = mfma32(f[2 * KSN * kb + i], qf[i], s[kb]);
+        if (kb == 0) {  // the next tile's copies, spread over the ops
+#pragma unroll
+          for (int j = 0; j < 2 * CPW; ++j)
+            if (j * KSN / (2 * CPW) == i) issue_j(j / 2, j % 2 == 0, kn, st ^ 1);
+        }
+        if (kb == 1 && i == 0)
+#pragma unroll
+          for (int e = 0; e < EP; ++e) form_p(0, (KSN - 1) * EP + e);
+        if (kb == 1 && i > 0)
+#pragma unroll
+          for (int e = 0; e < EP; ++e) form_ds(0, (i - 1) * EP + e);
+      }
+      if (kb == 1) {
+#pragma unroll
+        for (int e = 0; e < EP; ++e) form_ds(0, (KSN - 1) * EP + e);
+        sb[0] = operand(dp[0], 0);
+        sb[1] = operand(dp[0], 1);
+      }
+      if (k0 + 32 * kb + 32 > wave_all) {
+        sched_fence();
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kb][r] = k0 + 32 * kb + acc_row(r, hi) < klim ? s[kb][r] : -INFINITY;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dp[kb][r] = dd;  // dP - D
+#pragma unroll
+      for (int i = 0; i < KSN; ++i) {
+        sched_fence();
+        rd(2 * KSN * kb + KSN + i + PF);
+        dp[kb] = mfma32(f[2 * KSN * kb + KSN + i], dof[i], dp[kb]);
+        if (i > 0)
+#pragma unroll
+          for (int e = 0; e < EP; ++e) form_p(kb, (i - 1) * EP + e);
+      }
+    }
+    constexpr int ED = 16 / (2 * NB);
+#pragma unroll
+    for (int i = 0; i < 4 * NB; ++i) {
+      sched_fence();
+      rd(4 * KSN + i + PF);
+      acc[i % NB] = mfma32(g[i], sb[i / NB], acc[i % NB]);
+      if (i == 0)
+#pragma unroll
+        for (int e = 0; e < EP; ++e) form_p(1, (KSN - 1) * EP + e);
+      else if (i < 2 * NB)
+#pragma unroll
+        for (int e = 0; e < ED; ++e) form_ds(1, (i - 1) * ED + e);
+      if (i == 2 * NB - 1) {
+#pragma unroll
+        for (int e = 0; e < ED; ++e) form_ds(1, (2 * NB - 1) * ED + e);
+        sb[2] = operand(dp[1], 0);
+        sb[3] = operand(dp[1], 1);
+      }
+    }
+    sched_fence();
   }
   wait_all_memory();  // no copy outlives the workgroup
 
-  if (BIAS) {  // the block's sums per distance, waves in order
-    far_lo = wave_sum(far_lo);
-    far_hi = wave_sum(far_hi);
-    __syncthreads();
-    if (lane == 0) {
-      hist[w * HIST] += far_lo;
-      hist[w * HIST + 2 * a.R] += far_hi;
-    }
-    __syncthreads();
-    float* out = a.dist_part + (((size_t)it.s * a.nblk + it.blk) * a.H + it.h) * (2 * a.R + 1);
-    for (int i = tid; i < 2 * a.R + 1; i += 64 * kWaves) {
-      float x = 0.0f;
-      for (int j = 0; j < kWaves; ++j) x += hist[j * HIST + i];
-      out[i] = x;
-    }
+  // What dS of a row sums up to beside 0 is the error of its D, taken of the rounded O: the other
+  // pass gets D without it. (Rows past the sequence's own: inert.)
+  rowsum = halves_sum(rowsum);
+  if (hi == 0 && qi < ((sr.nq + 63) & ~63)) {
+    const size_t p = (size_t)it.h * a.npad + packed_row(sr.q0, it.s) + qi;
+    a.nls[p] = nls;
+    a.dd[p] = klim == 0 ? 0.0f : dd - rowsum;
   }
   if (qi < sr.sq) {  // rows that see no key, and rows of the slot past the sequence's own: 0
     __bf16* qp = a.dq + ((size_t)(sr.q0 + qi) * a.H + it.h) * D;
@@ -241,74 +292,118 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_dq_kernel(PackedArgs a)
   }
 }
 
-template <int D, bool BIAS>
-__global__ __launch_bounds__(64 * kWaves, 1) void packed_dkdv_kernel(PackedArgs a) {
+// A key block's steps: query tiles [t0, t0 + nt) of every query head of its group, heads in
+// order; a call of several chunks gives each workgroup a run of them; with a bias
+// there are as many chunks as heads, each of one head.
+struct KeySteps {
+  int t0, nt, u0, u1;
+};
+__device__ __forceinline__ KeySteps key_steps(const PackedArgs& a, const SeqRows& sr, int b0, int chunk) {
+  KeySteps k;
+  auto one = [](int x) { return __builtin_amdgcn_readfirstlane(x); };  // divided: back to a scalar register
+  // from the first query at or past the block's first key
+  k.t0 = (a.causal ? max(0, b0 - sr.off) : 0) / kBQ;
+  k.nt = b0 < sr.nk ? max(0, (sr.nq + kBQ - 1) / kBQ - k.t0) : 0;
+  k.u0 = one((int)((int64_t)a.G * k.nt * chunk / a.chunks));
+  k.u1 = one((int)((int64_t)a.G * k.nt * (chunk + 1) / a.chunks));
+  return k;
+}
+
+template <int D, int NW, bool BIAS>
+__global__ __launch_bounds__(64 * NW, 8 / NW) void packed_dkdv_kernel(PackedArgs a) {
   using Rows = SwzRows<D>;
   using Reads = SwzReads<D>;
+  constexpr int BM = 32 * NW;
   constexpr int RT = Rows::bytes(kBQ);
-  constexpr int STAGE = 2 * RT;                   // Q rows | dO rows
-  constexpr int COPIES = kBQ / Rows::RPC;
-  constexpr int STAT = 2 * STAGE;                 // -LSE/c[32] | -D[32] of a tile, two buffers
-  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE + 2 * 256];
+  constexpr int STAGE = 2 * RT;               // Q rows | dO rows of a tile
+  constexpr int COPIES = kBQ / Rows::RPC;     // wave copies of each
+  constexpr int CPW = 2 * COPIES / NW;        // copies per wave and tile, Q's first
+  constexpr int STAT = 2 * STAGE;             // -LSE/c | -D of a run of SQ queries, two buffers
+  constexpr int SQ = 256, SPT = SQ / kBQ;
+  constexpr int HIST = 2 * kMaxBiasDistance + 1;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE + 2 * 2 * SQ * 4];
   __shared__ float tb[BIAS ? kBiasTable : 1];
+  __shared__ float hist[BIAS ? NW * HIST : 1];  // each wave's sums of dS per distance inside (-R, R),
+  __shared__ float ends[BIAS ? NW * 128 : 1];   // each lane's of those up to -R and from R on
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l32 = lane & 31, hi = lane >> 5;
-  const int items = a.nblk * a.Hkv * a.S;
-  if ((int)blockIdx.x >= items) {  // rows outside every slot
-    const int wg = blockIdx.x - items, wgs = gridDim.x - items;
-    const int head = min(max(a.cu_k[0], 0), a.Tk), end = min(max(a.cu_k[a.S], head), a.Tk);
-    const int64_t per = (int64_t)a.Hkv * (D / 8);
-    for (int64_t i = (int64_t)wg * blockDim.x + tid; i < (head + a.Tk - end) * per; i += (int64_t)wgs * blockDim.x) {
-      const int r = (int)(i / per);
-      const size_t at = (size_t)(r < head ? r : r - head + end) * a.Hkv * D + i % per * 8;
-      *(bf16x8*)(a.dk + at) = zero_bf16x8();
-      *(bf16x8*)(a.dv + at) = zero_bf16x8();
-    }
+  const int items = a.nblk * a.Hkv * a.S * a.chunks;
+  if ((int)blockIdx.x >= items) {
+    clear_rows<D>(a.dk, a.dv, a.cu_k, a.S, a.Tk, a.Hkv, blockIdx.x - items, gridDim.x - items, tid, 64 * NW);
     return;
   }
-  // Under the causal rule the first key blocks are the longest: dispatched first.
+  // Key heads and sequences run fastest, then the chunks; the first key blocks, the longest
+  // under the causal rule, come first.
   const int HS = a.Hkv * a.S, kv = blockIdx.x % a.Hkv, seq = blockIdx.x / a.Hkv % a.S;
-  const int b0 = (int)(blockIdx.x / HS) * kBM;
+  const int chunk = blockIdx.x / HS % a.chunks, blk = blockIdx.x / HS / a.chunks;
+  const int b0 = blk * BM;
   const SeqRows sr = seq_rows(a, seq);
   if (b0 >= sr.sk) return;
-  const int key = b0 + w * 32 + l32;  // this lane's key
-  const bool valid = key < sr.nk;
-  // Query tiles that see the block's keys: from the first query at or past its first key.
-  const int first_q = a.causal ? max(0, b0 - sr.off) : 0;
-  const int t0 = first_q / kBQ, nt = b0 < sr.nk ? max(0, (sr.nq + kBQ - 1) / kBQ - t0) : 0;
-  const int steps = nt * a.G;
+  // Registers are the limit of the walk: what follows from the lane index is formed where it is
+  // used, from an index that the compiler must treat as new, and not held across the tiles.
+  auto fresh_lane = [&]() {
+    int x = lane;
+    asm volatile("" : "+v"(x));
+    return x;
+  };
+  auto lane_key = [&]() { return b0 + w * 32 + (fresh_lane() & 31); };  // this lane's key
+  const KeySteps ks = key_steps(a, sr, b0, chunk);
   const int wave_q = a.causal ? b0 + w * 32 - sr.off : 0;  // first query that sees a key of the wave
 
-  const __bf16* qbase = a.q + (size_t)sr.q0 * a.q_tok;
   const unsigned o_tok = a.H * D;
-  const __bf16* dbase = a.dout + (size_t)sr.q0 * o_tok;
+  const __bf16* qbase = a.q + (size_t)sr.q0 * a.q_tok + kv * a.G * D;
+  const __bf16* dbase = a.dout + (size_t)sr.q0 * o_tok + kv * a.G * D;
   const int srow = packed_row(sr.q0, seq);
-  auto copy_tile = [&](int u, int st) {
-    const int g = u / nt, q0 = (t0 + u % nt) * kBQ, h = kv * a.G + g;
-    const int idx = w % COPIES, first = swz_copy_row<D, true>(q0, sr.nq, idx);
-    VC_LDS char* dst = (VC_LDS char*)smem + st * STAGE + idx * Rows::GS;
-    if (D == 128 || w < COPIES)
-      copy16_to_lds_opaque(qbase + (size_t)first * a.q_tok + h * D, swz_copy_off<D, true>(first, a.q_tok, sr.nq, lane), dst);
-    if (D == 128 || w >= COPIES)
-      copy16_to_lds_opaque(dbase + (size_t)first * o_tok + h * D, swz_copy_off<D, true>(first, o_tok, sr.nq, lane), dst + RT);
-    if (w == 0) {
-      const size_t p = (size_t)h * a.npad + srow + q0 + l32;
-      ((VC_LDS float*)((VC_LDS char*)smem + STAT + st * 256))[lane] = hi ? a.dd[p] : a.nls[p];
-    }
+  // Copy j of this wave for the tile of query row q0, head g of the group, into stage st. Rows past nq repeat the last;
+  // their -LSE of -inf makes their probabilities zero.
+  auto copy_is_q = [&](int j) { return COPIES % NW == 0 ? j < COPIES / NW : w < COPIES; };
+  const __bf16* cbase[CPW];
+  unsigned ctok[CPW];
+#pragma unroll
+  for (int j = 0; j < CPW; ++j) {
+    cbase[j] = uniform_ptr(copy_is_q(j) ? qbase : dbase);
+    ctok[j] = __builtin_amdgcn_readfirstlane(copy_is_q(j) ? a.q_tok : o_tok);
+  }
+  auto issue_j = [&](int j, int g, int q0, int st) {
+    const int idx = (w + j * NW) % COPIES, first = swz_copy_row<D, true>(q0, sr.nq, idx);
+    copy16_to_lds_opaque(cbase[j] + (size_t)first * ctok[j] + g * D, swz_copy_off<D, true>(first, ctok[j], sr.nq, fresh_lane()),
+                         (VC_LDS char*)smem + st * STAGE + (copy_is_q(j) ? 0 : RT) + idx * Rows::GS);
+  };
+  // The row statistics of the run of SQ queries that holds tile t of head g, by the last two waves.
+  const float* sbase = uniform_ptr(w == NW - 2 ? a.nls : a.dd);
+  auto issue_stats = [&](int g, int t, int buf) {
+    if (w < NW - 2) return;
+    const bool is_l = w == NW - 2;
+    const size_t p = (size_t)(kv * a.G + g) * a.npad + srow + (ks.t0 + t / SPT * SPT) * kBQ;
+    copy16_to_lds_opaque(sbase + p, 16u * (unsigned)fresh_lane(),
+                         (VC_LDS char*)smem + STAT + buf * 2 * SQ * 4 + (is_l ? 0 : SQ * 4));
   };
 
+  int g = BIAS ? chunk : __builtin_amdgcn_readfirstlane(ks.nt ? ks.u0 / ks.nt : 0), t = ks.u0 - g * ks.nt, buf = 0;  // scalar, as u0
+  if (ks.u0 < ks.u1) {
+    issue_stats(g, t, 0);
+#pragma unroll
+    for (int j = 0; j < CPW; ++j) issue_j(j, g, (ks.t0 + t) * kBQ, 0);
+  }
   bf16x8 kf[D / 16], vf[D / 16];
   {
-    const size_t row = min(sr.k0 + min(key, max(sr.nk - 1, 0)), a.Tk - 1);
+    const size_t row = min(sr.k0 + min(lane_key(), max(sr.nk - 1, 0)), a.Tk - 1);
+    const int hi = lane >> 5;
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-      kf[ks] = *(const bf16x8*)(a.k + row * a.k_tok + kv * D + 16 * ks + 8 * hi);
-      vf[ks] = *(const bf16x8*)(a.v + row * a.v_tok + kv * D + 16 * ks + 8 * hi);
+    for (int i = 0; i < D / 16; ++i) {
+      kf[i] = *(const bf16x8*)(a.k + row * a.k_tok + kv * D + 16 * i + 8 * hi);
+      vf[i] = *(const bf16x8*)(a.v + row * a.v_tok + kv * D + 16 * i + 8 * hi);
     }
   }
+  if (BIAS) {
+    load_bias_table(a, kv * a.G + g, tb, tid, 64 * NW);
+    for (int i = tid; i < NW * HIST; i += 64 * NW) hist[i] = 0.0f;
+    for (int i = tid; i < NW * 128; i += 64 * NW) ends[i] = 0.0f;
+  }
+  wait_all_memory();  // the loads above too: no later wait stands among copies
+
   f32x16 dk_acc[D / 32], dv_acc[D / 32];
 #pragma unroll
   for (int i = 0; i < D / 32; ++i) {
@@ -316,77 +411,202 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_dkdv_kernel(PackedArgs 
     dv_acc[i] = zero_f32x16();
   }
   const int pos_k = b0 + w * 32;  // position of the wave's first key
-  if (steps > 0) copy_tile(0, 0);
-  for (int u = 0; u < steps; ++u) {
-    const int st = u & 1, g = u / nt, q0 = (t0 + u % nt) * kBQ;
+  for (int u = ks.u0; u < ks.u1; ++u) {
+    const int st = (u - ks.u0) & 1, q0 = (ks.t0 + t) * kBQ;
     wait_all_memory();
-    // dO rows past nq that this wave copied: zero, as a probability of 0 does not silence an
-    // infinite value of row nq - 1, which they repeat.
-    if (q0 + kBQ > sr.nq && (D == 128 || w >= COPIES)) {
-      const int idx = w % COPIES;
-      if (q0 + perm_row(Rows::RPC * idx + lane / Rows::CPR) >= sr.nq)
-        *(VC_LDS bf16x8*)((VC_LDS char*)smem + st * STAGE + RT + idx * Rows::GS + 16 * lane) = zero_bf16x8();
-    }
-    if (BIAS && u % nt == 0) {
-      __syncthreads();  // the previous head's table is no longer read
-      load_bias_table(a, kv * a.G + g, tb, tid, 64 * kWaves);
+    if (q0 + kBQ > sr.nq) {
+      // dO rows past nq that this wave copied: zero, as a probability of 0 does not silence an
+      // infinite value of the last row, which they repeat.
+#pragma unroll
+      for (int j = 0; j < CPW; ++j) {
+        const int idx = (w + j * NW) % COPIES, cl = fresh_lane();
+        f32x4 z = {0.0f, 0.0f, 0.0f, 0.0f};
+        asm volatile("" : "+v"(z));  // formed here: no registers hold it across the walk
+        if (!copy_is_q(j) && q0 + perm_row(Rows::RPC * idx + cl / Rows::CPR) >= sr.nq)
+          *(VC_LDS f32x4*)((VC_LDS char*)smem + st * STAGE + RT + idx * Rows::GS + 16 * cl) = z;
+      }
     }
     __syncthreads();
-    if (u + 1 < steps) copy_tile(u + 1, st ^ 1);
-    if (q0 + kBQ <= wave_q) continue;
-    const VC_LDS char* tile = (const VC_LDS char*)smem + st * STAGE;
-    const VC_LDS char* rp = tile + Reads::row_base(perm_row(l32), hi);
-    const VC_LDS char* tp = tile + Reads::tr_base(lane);
-    const VC_LDS float* stat = (const VC_LDS float*)((const VC_LDS char*)smem + STAT + st * 256) + 4 * hi;
-    f32x16 s, dp;
+    // The next step: the next tile, or the first one of the next head.
+    const bool last = u + 1 == ks.u1, turn = t + 1 == ks.nt;
+    const int gn = last ? g : turn ? g + 1 : g, tn = last ? t : turn ? 0 : t + 1;  // past the last: copied again, never read
+    const int qn = (ks.t0 + tn) * kBQ;
+    const int bufn = !last && tn % SPT == 0 ? buf ^ 1 : buf;
+    if (bufn != buf) issue_stats(gn, tn, bufn);
+    if (q0 + kBQ <= wave_q) {  // every query of the tile stands before the wave's keys
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const f32x4 nl = *(const VC_LDS f32x4*)(stat + 8 * j), nd = *(const VC_LDS f32x4*)(stat + 32 + 8 * j);
+      for (int j = 0; j < CPW; ++j) issue_j(j, gn, qn, st ^ 1);
+    } else {
+      // The tile's products in one stretch of matrix-core ops, every LDS operand read PF ops
+      // ahead, each phase's vector arithmetic between the ops of the next one: S = Q K^T;
+      // dP = -D + dO V^T while P is formed; dV^T += dO^T P while dS is formed; dK^T += Q^T dS.
+      constexpr int KSN = D / 16;
+      constexpr int NB = D / 32;
+      constexpr int PF = BIAS && D == 128 ? 1 : 2;  // the bias takes the registers of one operand
+      constexpr int EP = 16 / KSN;
+      constexpr int ED = 16 / (2 * NB);
+      const VC_LDS char* tile = (const VC_LDS char*)smem + st * STAGE;
+      const int ln = fresh_lane(), hi = ln >> 5;
+      const VC_LDS char* rp = tile + Reads::row_base(perm_row(ln & 31), hi);
+      const VC_LDS char* tp = tile + Reads::tr_base(ln);
+      const VC_LDS float* stat =
+          (const VC_LDS float*)((const VC_LDS char*)smem + STAT + buf * 2 * SQ * 4) + t % SPT * kBQ + 4 * hi;
+      f32x16 s, dp;
+      bf16x8 f[2 * KSN], gt[4 * NB];
+      auto rd = [&](int i) { f[i] = *(const VC_LDS bf16x8*)(Reads::row_at(rp, i % KSN) + (i < KSN ? 0 : RT)); };
+      auto rdt = [&](int i) { gt[i] = Reads::tr_operand(tp + (i < 2 * NB ? RT : 0), i / NB % 2, i % NB); };
+      float shift = 0.0f;
+      int side = 0;
+      auto form_p = [&](int r) { s[r] = fast_exp2(BIAS ? fmaf(s[r], a.scale_log2, shift) : s[r] * a.scale_log2); };
+      auto form_ds = [&](int r) { dp[r] = s[r] * dp[r]; };
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[4 * j + i] = nl[i];
-        dp[4 * j + i] = nd[i];
+      for (int i = 0; i < PF; ++i) rd(i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {  // S accumulates on top of -LSE/c, dP on top of -D of its query rows
+        const f32x4 nl = *(const VC_LDS f32x4*)(stat + 8 * j), nd = *(const VC_LDS f32x4*)(stat + SQ + 8 * j);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[4 * j + i] = nl[i];
+          dp[4 * j + i] = nd[i];
+        }
       }
-    }
-    float shift = 0.0f;
-    if (BIAS) {
-      const int side = bias_side(pos_k, pos_k + 31, q0 + sr.off, q0 + sr.off + 31, a.R);
-      if (side == 0) {
-        const float* t = tb + kBiasPad + a.R + (pos_k + l32 - q0 - sr.off - 4 * hi);
+      if (BIAS) {
+        side = bias_side(pos_k, pos_k + 31, q0 + sr.off, q0 + sr.off + 31, a.R);
+        if (side == 0) {
+          const float* b = tb + kBiasPad + a.R + (pos_k + (ln & 31) - q0 - sr.off - 4 * hi);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] += t[-(8 * (r >> 2) + (r & 3))];
-      } else {
-        shift = tb[kBiasPad + (side > 0 ? 2 * a.R : 0)] * a.scale_log2;
+          for (int r = 0; r < 16; ++r) s[r] += b[-(8 * (r >> 2) + (r & 3))];
+        } else {
+          shift = uniform(tb[kBiasPad + (side > 0 ? 2 * a.R : 0)] * a.scale_log2);
+        }
       }
-    }
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-      s = mfma32(*(const VC_LDS bf16x8*)Reads::row_at(rp, ks), kf[ks], s);
-      dp = mfma32(*(const VC_LDS bf16x8*)(Reads::row_at(rp, ks) + RT), vf[ks], dp);
-    }
-    if (a.causal && q0 < wave_q + 31) {  // queries before this lane's key
-      const int jmin = key - sr.off;
+      for (int i = 0; i < KSN; ++i) {
+        sched_fence();
+        rd(i + PF);
+        s = mfma32(f[i], kf[i], s);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = q0 + acc_row(r, hi) >= jmin ? s[r] : -INFINITY;
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] = fast_exp2(fmaf(s[r], a.scale_log2, shift));
-      dp[r] *= s[r];
-    }
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const bf16x8 pb = operand(s, half), sb = operand(dp, half);
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db) {
-        dv_acc[db] = mfma32(Reads::tr_operand(tp + RT, half, db), pb, dv_acc[db]);
-        dk_acc[db] = mfma32(Reads::tr_operand(tp, half, db), sb, dk_acc[db]);
+        for (int j = 0; j < CPW; ++j)
+          if (j * KSN / CPW == i) issue_j(j, gn, qn, st ^ 1);
       }
+      if (a.causal && q0 < wave_q + 31) {  // queries before this lane's key
+        sched_fence();
+        const int jmin = lane_key() - sr.off - q0 - 4 * (fresh_lane() >> 5);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = acc_row(r, 0) >= jmin ? s[r] : -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < KSN; ++i) {
+        sched_fence();
+        if (i + PF < KSN)
+          rd(KSN + i + PF);
+        else
+          rdt(i + PF - KSN);
+        dp = mfma32(f[KSN + i], vf[i], dp);
+        if (i > 0) {
+#pragma unroll
+          for (int e = 0; e < EP; ++e) form_p((i - 1) * EP + e);
+        }
+      }
+      bf16x8 pb[2], sb[2];
+      sched_fence();
+      pb[0] = operand(s, 0);
+#pragma unroll
+      for (int i = 0; i < 2 * NB; ++i) {
+        sched_fence();
+        rdt(i + PF);
+        dv_acc[i % NB] = mfma32(gt[i], pb[i / NB], dv_acc[i % NB]);
+        if (i == 0) {
+#pragma unroll
+          for (int e = 0; e < EP; ++e) form_p((KSN - 1) * EP + e);
+          pb[1] = operand(s, 1);
+        } else {
+#pragma unroll
+          for (int e = 0; e < ED; ++e) form_ds((i - 1) * ED + e);
+        }
+      }
+      sched_fence();
+      if (BIAS) {  // before dK's operands need the registers
+#pragma unroll
+        for (int e = 0; e < ED; ++e) form_ds((2 * NB - 1) * ED + e);
+        sb[1] = operand(dp, 1);
+      }
+      sb[0] = operand(dp, 0);
+      if (BIAS) {
+        const int fl = fresh_lane();
+        if (lane_key() >= sr.nk) {  // a key past the sequence's own has gone along with its last one
+#pragma unroll
+          for (int r = 0; r < 16; ++r) dp[r] = 0.0f;
+        }
+        if (side == 0) {
+          const float x = distance_sums(dp, fl);
+          const int d = pos_k - q0 - sr.off + (fl & 31) - 32 * (fl >> 5);
+          float* to = d <= -a.R ? ends + w * 128 + fl : d >= a.R ? ends + w * 128 + 64 + fl : hist + w * HIST + d + a.R;
+          *to += x;
+        } else {
+          float x = 0.0f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) x += dp[r];
+          ends[w * 128 + (side < 0 ? 0 : 64) + fl] += x;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * NB; ++i) {
+        sched_fence();
+        if (2 * NB + i + PF < 4 * NB) rdt(2 * NB + i + PF);
+        dk_acc[i % NB] = mfma32(gt[2 * NB + i], sb[i / NB], dk_acc[i % NB]);
+        if (!BIAS && i == 0) {
+#pragma unroll
+          for (int e = 0; e < ED; ++e) form_ds((2 * NB - 1) * ED + e);
+          sb[1] = operand(dp, 1);
+        }
+      }
+      sched_fence();
     }
+    g = gn;
+    t = tn;
+    buf = bufn;
   }
   wait_all_memory();  // no copy outlives the workgroup
+  if (BIAS) {  // the head's sums per distance, waves in order
+    const int ln = fresh_lane();
+    const float lo = wave_sum(ends[w * 128 + ln]), up = wave_sum(ends[w * 128 + 64 + ln]);
+    if (ln == 0) {
+      hist[w * HIST] += lo;
+      hist[w * HIST + 2 * a.R] += up;
+    }
+    __syncthreads();
+    float* out = a.dist_part + (((size_t)seq * a.nblk + blk) * a.H + kv * a.G + chunk) * (2 * a.R + 1);
+    for (int i = tid; i < 2 * a.R + 1; i += 64 * NW) {
+      float x = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NW; ++j) x += hist[j * HIST + i];
+      out[i] = x;
+    }
+  }
 
+  const int key = lane_key(), hi = fresh_lane() >> 5;
+  const bool valid = key < sr.nk;
   if (key < sr.sk) {  // rows of the slot past the sequence's own keys: exactly 0
+    if (a.chunks > 1) {
+      const size_t one = (size_t)a.Tk * a.Hkv * D;
+      float* pk = a.key_part + (size_t)chunk * 2 * one + ((size_t)(sr.k0 + key) * a.Hkv + kv) * D;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x16 &x = dk_acc[db], &y = dv_acc[db];
+          f32x4 tk, tv;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            tk[e] = valid ? x[4 * j + e] * a.scale : 0.0f;
+            tv[e] = valid ? y[4 * j + e] : 0.0f;
+          }
+          *(f32x4*)(pk + db * 32 + 8 * j + 4 * hi) = tk;
+          *(f32x4*)(pk + one + db * 32 + 8 * j + 4 * hi) = tv;
+        }
+      return;
+    }
     const size_t at = ((size_t)(sr.k0 + key) * a.Hkv + kv) * D;
     auto kr = [&](float x) { return (__bf16)(valid ? x * a.scale : 0.0f); };
     auto vr = [&](float x) { return (__bf16)(valid ? x : 0.0f); };
@@ -401,6 +621,22 @@ __global__ __launch_bounds__(64 * kWaves, 1) void packed_dkdv_kernel(PackedArgs 
   }
 }
 
+// dK, dV of every slot row as the sum of the chunks' partials, in order. One thread per 4 elements of each.
+__global__ __launch_bounds__(256) void packed_key_sum_kernel(PackedArgs a, int per_row) {
+  const int first = min(max(a.cu_k[0], 0), a.Tk), end = min(max(a.cu_k[a.S], first), a.Tk);
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x, one = (size_t)a.Tk * per_row;
+  const size_t at = (size_t)first * per_row + 4 * i;
+  if (at >= (size_t)end * per_row) return;
+  f32x4 sk = {0.0f, 0.0f, 0.0f, 0.0f}, sv = sk;
+#pragma unroll 4
+  for (int c = 0; c < a.chunks; ++c) {
+    sk += *(const f32x4*)(a.key_part + (size_t)c * 2 * one + at);
+    sv += *(const f32x4*)(a.key_part + ((size_t)c * 2 + 1) * one + at);
+  }
+  *(bf16x4*)(a.dk + at) = bf16x4{(__bf16)sk[0], (__bf16)sk[1], (__bf16)sk[2], (__bf16)sk[3]};
+  *(bf16x4*)(a.dv + at) = bf16x4{(__bf16)sv[0], (__bf16)sv[1], (__bf16)sv[2], (__bf16)sv[3]};
+}
+
 // Bias gradient: the row blocks' sums per distance added up in order (one workgroup per head),
 // then the distances of each bucket.
 __global__ __launch_bounds__(1024) void packed_dbias_kernel(PackedArgs a, __bf16* dbias) {
@@ -413,8 +649,9 @@ __global__ __launch_bounds__(1024) void packed_dbias_kernel(PackedArgs a, __bf16
     float x = 0.0f;
     if (g < groups && d < nd) {
       for (int i = g; i < a.S * a.nblk; i += groups) {
-        const SeqRows sr = seq_rows(a, i / a.nblk);
-        if (i % a.nblk * kBM < sr.sq) x += a.dist_part[((size_t)i * a.H + h) * nd + d];
+        const int s = i / a.nblk, k0 = min(max(a.cu_k[s], 0), a.Tk);  // blocks inside the slot have sums
+        const int sk = min(min(max(a.cu_k[s + 1], k0), a.Tk) - k0, a.max_k);
+        if (i % a.nblk * a.bm < sk) x += a.dist_part[((size_t)i * a.H + h) * nd + d];
       }
     }
     part[tid] = x;
@@ -435,31 +672,41 @@ __global__ __launch_bounds__(1024) void packed_dbias_kernel(PackedArgs a, __bf16
 
 }  // namespace
 
-hipError_t launch_packed_bwd(const PackedArgs& args, int head_dim, __bf16* dbias, hipStream_t s) {
-  PackedArgs a = args;
+namespace {
+template <int D, int NW, bool BIAS>
+void launch_bwd(PackedArgs a, __bf16* dbias, int clear, hipStream_t s) {
+  constexpr int BM = 32 * NW;
+  const dim3 block(64 * NW);
+  a.bm = BM;
+  a.nblk = (a.max_q + BM - 1) / BM;
+  hipLaunchKernelGGL((packed_dq_kernel<D, NW, BIAS>), dim3(a.nblk * a.H * a.S + clear), block, 0, s, a);
+  a.nblk = (a.max_k + BM - 1) / BM;
+  hipLaunchKernelGGL((packed_dkdv_kernel<D, NW, BIAS>), dim3(a.nblk * a.Hkv * a.S * a.chunks + clear), block, 0, s, a);
+  if (a.chunks > 1) {
+    const size_t threads = (size_t)a.Tk * a.Hkv * D / 4;
+    hipLaunchKernelGGL(packed_key_sum_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, a.Hkv * D);
+  }
+  if (BIAS && dbias) hipLaunchKernelGGL(packed_dbias_kernel, dim3(a.H), dim3(1024), 0, s, a, dbias);
+}
+}  // namespace
+
+hipError_t launch_packed_bwd(const PackedArgs& a, int head_dim, __bf16* dbias, hipStream_t s) {
   const int clear = a.clear ? 32 : 0;
-  const dim3 block(64 * kWaves);
-  a.nblk = (a.max_q + kBM - 1) / kBM;
-  const dim3 qgrid(a.nblk * a.H * a.S + clear);
+  auto go = [&](auto d, auto bias) {
+    if (a.small)
+      launch_bwd<decltype(d)::value, 4, decltype(bias)::value>(a, dbias, clear, s);
+    else
+      launch_bwd<decltype(d)::value, 8, decltype(bias)::value>(a, dbias, clear, s);
+  };
+  using std::integral_constant;
   if (head_dim == 128 && a.bias)
-    hipLaunchKernelGGL((packed_dq_kernel<128, true>), qgrid, block, 0, s, a);
+    go(integral_constant<int, 128>{}, std::true_type{});
   else if (head_dim == 128)
-    hipLaunchKernelGGL((packed_dq_kernel<128, false>), qgrid, block, 0, s, a);
+    go(integral_constant<int, 128>{}, std::false_type{});
   else if (a.bias)
-    hipLaunchKernelGGL((packed_dq_kernel<64, true>), qgrid, block, 0, s, a);
+    go(integral_constant<int, 64>{}, std::true_type{});
   else
-    hipLaunchKernelGGL((packed_dq_kernel<64, false>), qgrid, block, 0, s, a);
-  if (dbias) hipLaunchKernelGGL(packed_dbias_kernel, dim3(a.H), dim3(1024), 0, s, a, dbias);
-  a.nblk = (a.max_k + kBM - 1) / kBM;
-  const dim3 kgrid(a.nblk * a.Hkv * a.S + clear);
-  if (head_dim == 128 && a.bias)
-    hipLaunchKernelGGL((packed_dkdv_kernel<128, true>), kgrid, block, 0, s, a);
-  else if (head_dim == 128)
-    hipLaunchKernelGGL((packed_dkdv_kernel<128, false>), kgrid, block, 0, s, a);
-  else if (a.bias)
-    hipLaunchKernelGGL((packed_dkdv_kernel<64, true>), kgrid, block, 0, s, a);
-  else
-    hipLaunchKernelGGL((packed_dkdv_kernel<64, false>), kgrid, block, 0, s, a);
+    go(integral_constant<int, 64>{}, std::false_type{});
   return hipGetLastError();
 }
 

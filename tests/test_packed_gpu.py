@@ -245,6 +245,14 @@ def test_many_sequences():
     check(*make(21, lens, lens, 2, 2, 64, False, 12, 33))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [False, True], ids=["full", "causal"])
+@pytest.mark.parametrize("nb", [0, 16])
+def test_longer_sequences(nb, causal, D):
+    """Slots of more than 2,048 rows (wider blocks), a sequence that ends inside one, and a short one beside it."""
+    check(*make(28, [2100, 70, 1], [2100, 300, 1], 2, 1 if nb == 0 else 2, D, causal, nb, 100 if nb else 0))
+
+
 def test_reproducible():
     """Two runs agree bitwise."""
     import torch
