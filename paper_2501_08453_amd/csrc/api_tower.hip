@@ -17,6 +17,7 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 inline const __bf16* bf(const void* p) { return static_cast<const __bf16*>(p); }
 
+constexpr int64_t kMaxGrid = (int64_t)1 << 30;    // workgroups of one launch
 constexpr int64_t kMaxRows = (int64_t)1 << 30;
 constexpr int64_t kMaxStride = (int64_t)1 << 23;  // elements between tokens: tile offsets of 16 rows stay in 32 bits
 
@@ -89,6 +90,34 @@ vcja::PackedArgs packed_args(const vc_packedattn_desc* d, const void* q, const v
   return a;
 }
 
+// Forward: heads of a group packed into a row block, workgroups of four or eight waves, and the
+// chunks of a row block's key tiles.
+struct FwdPlan {
+  int pack, chunks, span;
+  bool small;
+};
+FwdPlan fwd_plan(const vc_packedattn_desc* d) {
+  const int group = d->heads / d->kv_heads;
+  FwdPlan p;
+  p.pack = !d->num_buckets && (int64_t)d->max_q * group <= 128 ? group : 1;
+  const int64_t rows = (int64_t)d->max_q * p.pack;
+  p.small = rows <= 2048;
+  const int bm = p.small ? 128 : 256;
+  const int64_t blocks = std::min<int64_t>(d->sequences * ((rows + bm - 1) / bm), d->total_q * p.pack / bm + d->sequences) *
+                         (d->heads / p.pack);
+  const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
+  const int64_t want = blocks >= 512 ? 1 : (1024 + blocks - 1) / blocks;
+  const int64_t grid = d->sequences * ((rows + bm - 1) / bm) * (d->heads / p.pack);
+  p.chunks = (int)std::max<int64_t>(1, std::min({want, (int64_t)ntile / 8, kMaxGrid / grid}));
+  p.span = (ntile + p.chunks - 1) / p.chunks;
+  p.chunks = (ntile + p.span - 1) / p.span;
+  return p;
+}
+size_t fwd_part_bytes(const vc_packedattn_desc* d) {
+  const FwdPlan p = fwd_plan(d);
+  return p.chunks == 1 ? 256 : align256((size_t)p.chunks * d->total_q * d->heads * (d->head_dim + 2) * sizeof(float));
+}
+
 // Backward workspace: -LSE/c | -D | the bias gradient's sums per distance.
 size_t stat_bytes(const vc_packedattn_desc* d) {
   return align256((size_t)d->heads * vcja::packed_rows(d->total_q, d->sequences) * sizeof(float));
@@ -101,7 +130,8 @@ int key_chunks(const vc_packedattn_desc* d) {
   const int64_t blocks = std::min<int64_t>((int64_t)d->sequences * ((d->max_k + bm - 1) / bm), d->total_k / bm + d->sequences);
   const int64_t want = (1024 + d->kv_heads * blocks - 1) / (d->kv_heads * blocks);
   const int64_t steps = (int64_t)group * ((d->max_q + 31) / 32);
-  return (int)std::max<int64_t>(1, std::min(want, steps / 8));
+  const int64_t grid = (int64_t)d->sequences * ((d->max_k + bm - 1) / bm) * d->kv_heads;
+  return (int)std::max<int64_t>(1, std::min({want, steps / 8, kMaxGrid / grid}));
 }
 size_t dist_bytes(const vc_packedattn_desc* d) {
   if (!d->num_buckets) return 0;
@@ -134,7 +164,7 @@ vc_status check_ws(const void* ws, size_t have, size_t need) {
 extern "C" {
 
 size_t vc_packedattn_fwd_workspace_bytes(const vc_packedattn_desc* desc) {
-  return check_packed(desc) == VC_OK ? 256 : 0;
+  return check_packed(desc) == VC_OK ? fwd_part_bytes(desc) : 0;
 }
 
 vc_status vc_packedattn_fwd(const vc_packedattn_desc* desc, const void* q, const void* k, const void* v,
@@ -151,6 +181,12 @@ vc_status vc_packedattn_fwd(const vc_packedattn_desc* desc, const void* q, const
   vcja::PackedArgs a = packed_args(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets);
   a.o = static_cast<__bf16*>(o);
   a.lse = lse;
+  const FwdPlan p = fwd_plan(desc);
+  a.pack = p.pack;
+  a.chunks = p.chunks;
+  a.span = p.span;
+  a.small = p.small;
+  a.part = static_cast<float*>(workspace);
   return vcja::launch_packed_fwd(a, desc->head_dim, as_stream(stream)) == hipSuccess ? VC_OK : VC_ERR_HIP;
 }
 

@@ -29,7 +29,9 @@ struct PackedArgs {
   float scale, scale_log2;  // softmax scale; times log2(e)
   int nblk, bm;             // row blocks of the longest slot, rows of one
   bool small;               // workgroups of four waves instead of eight
-  int chunks;               // backward: workgroups that share a key block's query tiles
+  int chunks;               // workgroups that share a row block's key tiles (backward: a key block's query tiles)
+  int pack, span;           // forward: heads of a group in one row block; key tiles of a chunk
+  float* part;              // forward: the chunks' partial results (see write_partial)
   float* key_part;          // their partial dK, dV: [chunks][2][Tk, Hkv, D]
   // Backward: per query row -LSE / c (-inf on padding) and -D, [H, npad], sequence s from row
   // packed_row(cu_q[s], s) on.
