@@ -99,24 +99,20 @@ def relative_buckets(num_buckets, max_distance, bidirectional=True, device="cuda
     return torch.tensor(side[:0:-1] + [0] + ahead, dtype=torch.int32, device=device)
 
 
-class _OnDevice:
-    """Makes `device` current for a call (the library launches on the current device) unless it is already."""
-
-    def __init__(self, device):
-        import torch
-        self._d = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self._d is not None:
-            self._d.__enter__()
-
-    def __exit__(self, *exc):
-        if self._d is not None:
-            self._d.__exit__(*exc)
+def _launch(device, f, *args):
+    """f(*args) with `device` current (the library launches on the current device)."""
+    import torch
+    if device.index == torch.cuda.current_device():
+        return f(*args)
+    with torch.cuda.device(device):
+        return f(*args)
 
 
 def _token_stride(name, t):
-    """Elements between the rows of consecutive tokens of a [tokens, heads, D] tensor whose heads are contiguous."""
+    """Elements between the rows of consecutive tokens of a [tokens, heads, D] tensor whose heads are contiguous; 0
+    where the whole tensor is."""
+    if t.is_contiguous():
+        return 0
     n, h, d = t.shape
     if t.stride(2) != 1 or (h > 1 and t.stride(1) != d):
         raise ValueError("the heads of %s must be contiguous" % name)
@@ -127,39 +123,59 @@ def _token_stride(name, t):
     return t.stride(0)
 
 
-def _check_packed(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets, rows=()):
+def _fits(t, shape, dtype, index, strided=False):
+    return t.shape == shape and t.dtype is dtype and t.get_device() == index and (strided or t.is_contiguous())
+
+
+def _check_all(every):
+    """every: (name, tensor, shape, dtype, strided) of one call; all on one GPU, contiguous unless strided. The plain
+    comparisons first, as they cost a small call as much as its launch; what is wrong is then found out in the
+    order of the package's checks: shapes and dtypes of all, then where they lie."""
+    index = every[0][1].get_device()
+    if index >= 0:
+        for _, t, shape, dtype, strided in every:
+            if not _fits(t, shape, dtype, index, strided):
+                break
+        else:
+            return
+    for name, t, shape, dtype, _ in every:
+        _check_shape(name, t, shape, dtype)
+    for name, t, _, _, strided in every:
+        if t.device.type != "cuda":
+            raise ValueError("%s must be on a GPU" % name)
+        if t.device != every[0][1].device:
+            raise ValueError("%s is on %s, %s on %s" % (name, t.device, every[0][0], every[0][1].device))
+        if not strided:
+            _check_placed(name, t)
+
+
+def _check_packed(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets, like_q, like_k, lse):
     """Checks the tensors of one call against each other and the descriptor; returns a copy of the descriptor with
-    the tensors' strides. rows: further (name, tensor, dtype) with the shape of q (lse: [heads, total_q])."""
+    the tensors' strides. like_q, like_k: further (name, tensor) with the shape of q (of k)."""
     import torch
     bf16, i32 = torch.bfloat16, torch.int32
-    d = desc
-    every = [("q", q, (d.total_q, d.heads, d.head_dim), bf16), ("k", k, (d.total_k, d.kv_heads, d.head_dim), bf16),
-             ("v", v, (d.total_k, d.kv_heads, d.head_dim), bf16), ("cu_q", cu_q, (d.sequences + 1,), i32),
-             ("cu_k", cu_k, (d.sequences + 1,), i32)]
-    for name, t in (("len_q", len_q), ("len_k", len_k)):
-        if t is not None:
-            every.append((name, t, (d.sequences,), i32))
+    d = vc_packedattn_desc.from_buffer_copy(desc)
+    S, H, D = d.sequences, d.heads, d.head_dim
     if (d.num_buckets > 0) != (bias is not None) or (bias is None) != (buckets is None):
         raise ValueError("a bias and its buckets go with a descriptor of num_buckets > 0, and only with that")
+    sq, sk = (d.total_q, H, D), (d.total_k, d.kv_heads, D)
+    every = [("q", q, sq, bf16, True), ("k", k, sk, bf16, True), ("v", v, sk, bf16, True), ("cu_q", cu_q, (S + 1,), i32, False),
+             ("cu_k", cu_k, (S + 1,), i32, False)]
+    if len_q is not None:
+        every.append(("len_q", len_q, (S,), i32, False))
+    if len_k is not None:
+        every.append(("len_k", len_k, (S,), i32, False))
     if bias is not None:
-        every += [("bias", bias, (d.heads, d.num_buckets), bf16), ("buckets", buckets, (2 * d.max_distance + 1,), i32)]
-    for name, t in rows:
-        lse = name == "lse"
-        like = (d.total_k, d.kv_heads, d.head_dim) if name in ("dk", "dv") else (d.total_q, d.heads, d.head_dim)
-        every.append((name, t, (d.heads, d.total_q) if lse else like, torch.float32 if lse else bf16))
-    for name, t, shape, dtype in every:
-        _check_shape(name, t, shape, dtype)
-    for name, t, _, _ in every:
-        if t.device != q.device:
-            raise ValueError("%s is on %s, q on %s" % (name, t.device, q.device))
-        if name in ("q", "k", "v"):
-            if t.device.type != "cuda":
-                raise ValueError("%s must be on a GPU" % name)
-        else:
-            _check_placed(name, t)
-    out = vc_packedattn_desc.from_buffer_copy(d)
-    out.q_stride, out.k_stride, out.v_stride = _token_stride("q", q), _token_stride("k", k), _token_stride("v", v)
-    return out
+        every.append(("bias", bias, (H, d.num_buckets), bf16, False))
+        every.append(("buckets", buckets, (2 * d.max_distance + 1,), i32, False))
+    for name, t in like_q:
+        every.append((name, t, sq, bf16, False))
+    for name, t in like_k:
+        every.append((name, t, sk, bf16, False))
+    every.append(("lse", lse, (H, d.total_q), torch.float32, False))
+    _check_all(every)
+    d.q_stride, d.k_stride, d.v_stride = _token_stride("q", q), _token_stride("k", k), _token_stride("v", v)
+    return d
 
 
 def packed_fwd(q, k, v, desc, cu_q, cu_k, len_q=None, len_k=None, bias=None, buckets=None, out=None, lse=None, ws=None):
@@ -171,11 +187,10 @@ def packed_fwd(q, k, v, desc, cu_q, cu_k, len_q=None, len_k=None, bias=None, buc
     made = out is None
     out = torch.empty((desc.total_q, desc.heads, desc.head_dim), dtype=torch.bfloat16, device=q.device) if made else out
     lse = torch.empty((desc.heads, desc.total_q), dtype=torch.float32, device=q.device) if lse is None else lse
-    d = _check_packed(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets, (("out", out), ("lse", lse)))
+    d = _check_packed(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets, (("out", out),), (), lse)
     d.clear_outside = 1 if made else 0
-    with _OnDevice(q.device):
-        ws = packed_fwd_workspace(d, q.device) if ws is None else ws
-        vc_packedattn_fwd(d, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets, out, lse, ws, ws.numel())
+    ws = packed_fwd_workspace(d, q.device) if ws is None else ws
+    _launch(q.device, vc_packedattn_fwd, d, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets, out, lse, ws, ws.numel())
     return out, lse
 
 
@@ -192,12 +207,12 @@ def packed_bwd(q, k, v, o, lse, dout, desc, cu_q, cu_k, len_q=None, len_k=None, 
         new = lambda n, h: torch.empty((n, h, desc.head_dim), dtype=torch.bfloat16, device=q.device)  # noqa: E731
         dq, dk, dv = new(desc.total_q, desc.heads), new(desc.total_k, desc.kv_heads), new(desc.total_k, desc.kv_heads)
     d = _check_packed(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets,
-                      (("o", o), ("lse", lse), ("dout", dout), ("dq", dq), ("dk", dk), ("dv", dv)))
+                      (("o", o), ("dout", dout), ("dq", dq)), (("dk", dk), ("dv", dv)), lse)
     d.clear_outside = 1 if made else 0
     dbias = torch.empty_like(bias) if bias is not None and want_dbias else None
-    with _OnDevice(q.device):
-        ws = packed_bwd_workspace(d, q.device) if ws is None else ws
-        vc_packedattn_bwd(d, q, k, v, o, lse, dout, cu_q, cu_k, len_q, len_k, bias, buckets, dq, dk, dv, dbias, ws, ws.numel())
+    ws = packed_bwd_workspace(d, q.device) if ws is None else ws
+    _launch(q.device, vc_packedattn_bwd, d, q, k, v, o, lse, dout, cu_q, cu_k, len_q, len_k, bias, buckets, dq, dk, dv, dbias,
+            ws, ws.numel())
     return dq, dk, dv, dbias
 
 
@@ -214,56 +229,60 @@ def _row_stride(name, t):
     raise ValueError("%s must be contiguous, or two-dimensional with contiguous rows" % name)
 
 
-def _norm_desc(x, weight, bias, eps, dout=None, stats=(), outs=()):
+def _norm_desc(x, weight, bias, eps, dout=None, mean=None, rstd=None, out=None):
     import torch
-    types = {torch.bfloat16: 0, torch.float32: 1}
-    if x.dtype not in types:
+    if x.dtype is not torch.bfloat16 and x.dtype is not torch.float32:
         raise ValueError("x must be torch.bfloat16 or torch.float32, got %s" % x.dtype)
-    if x.dim() < 1 or x.shape[-1] < 1:
-        raise ValueError("x has shape %s, expected [..., columns]" % (tuple(x.shape),))
-    params = [(n, t) for n, t in (("weight", weight), ("bias", bias)) if t is not None]
-    for n, t in params:
-        if t.dtype not in types or t.dtype != params[0][1].dtype:
-            raise ValueError("weight and bias must be both torch.bfloat16 or both torch.float32, got %s" % t.dtype)
-    every = [(n, t, (x.shape[-1],), t.dtype) for n, t in params]
-    every += [(n, t, x.shape[:-1], torch.float32) for n, t in stats] + [(n, t, x.shape, x.dtype) for n, t in outs]
-    for n, t, shape, dtype in every + ([("dout", dout, x.shape, x.dtype)] if dout is not None else []):
-        _check_shape(n, t, shape, dtype)
-        if t.device != x.device:
-            raise ValueError("%s is on %s, x on %s" % (n, t.device, x.device))
-    if x.device.type != "cuda":
-        raise ValueError("x must be on a GPU")
-    for n, t, _, _ in every:
-        _check_placed(n, t)
-    return vc_layernorm_desc(x.numel() // x.shape[-1], x.shape[-1], types[x.dtype], types[params[0][1].dtype] if params else 0,
-                             float(eps), _row_stride("x", x), 0 if dout is None else _row_stride("dout", dout))
+    shape = x.shape
+    if not shape or shape[-1] < 1:
+        raise ValueError("x has shape %s, expected [..., columns]" % (tuple(shape),))
+    cols = shape[-1]
+    first = weight if weight is not None else bias
+    if first is not None and first.dtype is not torch.bfloat16 and first.dtype is not torch.float32:
+        raise ValueError("weight and bias must be torch.bfloat16 or torch.float32, got %s" % first.dtype)
+    if weight is not None and bias is not None and bias.dtype is not weight.dtype:
+        raise ValueError("weight and bias must be of one dtype, got %s and %s" % (weight.dtype, bias.dtype))
+    every = [("x", x, shape, x.dtype, True)]
+    if weight is not None:
+        every.append(("weight", weight, (cols,), first.dtype, False))
+    if bias is not None:
+        every.append(("bias", bias, (cols,), first.dtype, False))
+    if dout is not None:
+        every.append(("dout", dout, shape, x.dtype, True))
+        every.append(("mean", mean, shape[:-1], torch.float32, False))
+        every.append(("rstd", rstd, shape[:-1], torch.float32, False))
+    if out is not None:
+        every.append(("out", out, shape, x.dtype, False))
+    _check_all(every)
+    return vc_layernorm_desc(x.numel() // cols, cols, 1 if x.dtype is torch.float32 else 0,
+                             1 if first is not None and first.dtype is torch.float32 else 0, eps, _row_stride("x", x),
+                             0 if dout is None else _row_stride("dout", dout))
 
 
 def layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None):
     """(y, mean, rstd): layer norm over the last dimension of x (bf16 or fp32; contiguous, or [rows, columns] with
     rows further apart). weight and bias: [columns] in bf16 or fp32. mean and rstd are fp32, for the backward."""
     import torch
+    desc = _norm_desc(x, weight, bias, eps, out=out)
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    mean, rstd = (torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device) for _ in range(2))
-    desc = _norm_desc(x, weight, bias, eps, outs=(("out", y),))
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    rstd = torch.empty_like(mean)
     if desc.rows:
-        with _OnDevice(x.device):
-            vc_layernorm_fwd(desc, x, weight, bias, y, mean, rstd)
+        _launch(x.device, vc_layernorm_fwd, desc, x, weight, bias, y, mean, rstd)
     return y, mean, rstd
 
 
 def layer_norm_bwd(dout, x, weight, bias, mean, rstd, ws=None):
     """(dx, dweight, dbias) from the forward's inputs, mean and rstd; dweight (dbias) is None where weight (bias) is."""
     import torch
-    desc = _norm_desc(x, weight, bias, 0.0, dout, (("mean", mean), ("rstd", rstd)))
+    desc = _norm_desc(x, weight, bias, 0.0, dout, mean, rstd)
     dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     new = torch.empty_like if desc.rows else torch.zeros_like
     dw, db = (None if t is None else new(t) for t in (weight, bias))
     if desc.rows:
-        with _OnDevice(x.device):
-            if ws is None and (dw is not None or db is not None):
-                ws = _workspace(vc_layernorm_bwd_workspace_bytes(desc), x.device)
-            vc_layernorm_bwd(desc, dout, x, weight, mean, rstd, dx, dw, db, ws, 0 if ws is None else ws.numel())
+        if ws is None and (dw is not None or db is not None):
+            ws = _workspace(vc_layernorm_bwd_workspace_bytes(desc), x.device)
+        _launch(x.device, vc_layernorm_bwd, desc, dout, x, weight, mean, rstd, dx, dw, db, ws, 0 if ws is None else ws.numel())
     return dx, dw, db
 
 
