@@ -136,7 +136,7 @@ int key_chunks(const vc_packedattn_desc* d) {
 size_t dist_bytes(const vc_packedattn_desc* d) {
   if (!d->num_buckets) return 0;
   const int bm = small_blocks(d) ? 128 : 256;
-  return align256((size_t)d->sequences * ((d->max_k + bm - 1) / bm) * d->heads * (2 * d->max_distance + 1) * sizeof(float));
+  return align256((size_t)(vcja::dist_row(d->total_k, d->sequences, 0, bm) + 1) * d->heads * (2 * d->max_distance + 1) * sizeof(float));
 }
 size_t key_part_bytes(const vc_packedattn_desc* d) {
   const int c = key_chunks(d);

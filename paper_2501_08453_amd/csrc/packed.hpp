@@ -37,7 +37,7 @@ struct PackedArgs {
   // packed_row(cu_q[s], s) on.
   float *nls, *dd;
   int npad;
-  float* dist_part;         // bias gradient: per (sequence, row block, head) the sums per distance
+  float* dist_part;         // bias gradient: sums per distance, [dist_row][H][2 R + 1]
 };
 
 // A pointer that is the same for the whole wave, in scalar registers.
@@ -82,7 +82,12 @@ __device__ __forceinline__ int query_row(const PackedArgs& a, const SeqRows& r, 
 __host__ __device__ constexpr int packed_row(int q0, int s) { return ((q0 + 63) & ~63) + 64 * s; }
 __host__ __device__ constexpr int64_t packed_rows(int64_t Tq, int64_t S) { return ((Tq + 63) & ~(int64_t)63) + 64 * (S + 1) + 256; }
 
-// Sums and offsets of one (row block, head, sequence) item of a 1-D grid: heads and sequences
+// Row of the bias gradient's per-distance sums for block `blk` (of bm keys) of the sequence whose
+// keys start at k0: a sequence's blocks lie one behind the other, at most Tk / bm + S rows in all, and
+// a sequence's rows end at or before the next one's first. (Rows between: zeros.)
+__host__ __device__ constexpr int64_t dist_row(int64_t k0, int s, int blk, int bm) { return k0 / bm + s + blk; }
+
+// Position of one (row block, head, sequence) item of a 1-D grid: heads and sequences
 // run fastest, key heads before the query heads of a group, so that (with 8 key heads or a
 // multiple) the workgroups that read a key head's rows sit on one XCD; the last row blocks, the
 // longest under the causal rule, are dispatched first.

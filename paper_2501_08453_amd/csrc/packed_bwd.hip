@@ -122,6 +122,7 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void packed_dq_kernel(PackedArgs a
     }
   };
 
+  if (ntile > 0) issue_tile(0, 0);  // in flight with the loads below
   bf16x8 qf[D / 16], dof[D / 16];
   float nls, dd;
   {
@@ -150,7 +151,6 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void packed_dq_kernel(PackedArgs a
   const float nlse2 = nls * a.scale_log2;
   float rowsum = 0.0f;
 
-  if (ntile > 0) issue_tile(0, 0);
   wait_all_memory();  // the loads above too: no later wait stands among copies
   for (int kt = 0; kt < ntile; ++kt) {
     const int st = kt & 1;
@@ -340,6 +340,13 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void packed_dkdv_kernel(PackedArgs
   const int chunk = blockIdx.x / HS % a.chunks, blk = blockIdx.x / HS / a.chunks;
   const int b0 = blk * BM;
   const SeqRows sr = seq_rows(a, seq);
+  if (BIAS && b0 + BM >= sr.sk && (b0 < sr.sk || blk == 0)) {
+    // the sequence's last block (or an empty slot): no sums in the rows up to the next sequence's
+    const int64_t r0 = dist_row(sr.k0, seq, b0 < sr.sk ? blk + 1 : 0, BM);
+    const int64_t r1 = dist_row(min(max(__builtin_amdgcn_readfirstlane(a.cu_k[seq + 1]), 0), a.Tk), seq + 1, 0, BM);
+    for (int64_t r = r0; r < r1; ++r)
+      for (int i = tid; i < 2 * a.R + 1; i += 64 * NW) a.dist_part[(r * a.H + kv * a.G + chunk) * (2 * a.R + 1) + i] = 0.0f;
+  }
   if (b0 >= sr.sk) return;
   // Registers are the limit of the walk: what follows from the lane index is formed where it is
   // used, from an index that the compiler must treat as new, and not held across the tiles.
@@ -576,7 +583,7 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void packed_dkdv_kernel(PackedArgs
       hist[w * HIST + 2 * a.R] += up;
     }
     __syncthreads();
-    float* out = a.dist_part + (((size_t)seq * a.nblk + blk) * a.H + kv * a.G + chunk) * (2 * a.R + 1);
+    float* out = a.dist_part + (dist_row(sr.k0, seq, blk, BM) * a.H + kv * a.G + chunk) * (2 * a.R + 1);
     for (int i = tid; i < 2 * a.R + 1; i += 64 * NW) {
       float x = 0.0f;
 #pragma unroll
@@ -637,36 +644,50 @@ __global__ __launch_bounds__(256) void packed_key_sum_kernel(PackedArgs a, int p
   *(bf16x4*)(a.dv + at) = bf16x4{(__bf16)sv[0], (__bf16)sv[1], (__bf16)sv[2], (__bf16)sv[3]};
 }
 
-// Bias gradient: the row blocks' sums per distance added up in order (one workgroup per head),
-// then the distances of each bucket.
+// Bias gradient, one workgroup per head: the blocks' sums per distance added up in order, then
+// the distances of each bucket. In both steps the threads share the sums of one result by runs,
+// which are then joined in order.
 __global__ __launch_bounds__(1024) void packed_dbias_kernel(PackedArgs a, __bf16* dbias) {
   __shared__ float part[1024];
   __shared__ float sum[2 * kMaxBiasDistance + 1];
+  __shared__ int bucket[2 * kMaxBiasDistance + 1];
   const int h = blockIdx.x, nd = 2 * a.R + 1, tid = threadIdx.x;
-  const int groups = max(1, 1024 / nd), per = min(nd, 1024);  // threads: `groups` runs of blocks x distances
-  for (int d0 = 0; d0 < nd; d0 += per) {
-    const int d = d0 + tid % per, g = tid / per;
+  for (int d = tid; d < nd; d += 1024) bucket[d] = a.buckets[d];
+  const int r0 = (int)dist_row(min(max(a.cu_k[0], 0), a.Tk), 0, 0, a.bm);
+  const int r1 = (int)dist_row(min(max(a.cu_k[a.S], 0), a.Tk), a.S, 0, a.bm);
+  const float* rows = a.dist_part + (size_t)h * nd;
+  const size_t one = (size_t)a.H * nd;
+  for (int d0 = 0; d0 < nd; d0 += 1024) {
+    const int n = min(nd - d0, 1024), runs = 1024 / n, run = tid / n, d = d0 + tid % n;
     float x = 0.0f;
-    if (g < groups && d < nd) {
-      for (int i = g; i < a.S * a.nblk; i += groups) {
-        const int s = i / a.nblk, k0 = min(max(a.cu_k[s], 0), a.Tk);  // blocks inside the slot have sums
-        const int sk = min(min(max(a.cu_k[s + 1], k0), a.Tk) - k0, a.max_k);
-        if (i % a.nblk * a.bm < sk) x += a.dist_part[((size_t)i * a.H + h) * nd + d];
-      }
+    if (run < runs) {
+#pragma unroll 8
+      for (int r = r0 + run; r < r1; r += runs) x += rows[r * one + d];
     }
     part[tid] = x;
     __syncthreads();
-    if (tid < per && d < nd) {
-      float y = 0.0f;
-      for (int j = 0; j < groups; ++j) y += part[j * per + tid];
-      sum[d] = y;
+    if (tid < n) {
+      x = 0.0f;
+      for (int i = 0; i < runs; ++i) x += part[i * n + tid];
+      sum[d] = x;
     }
     __syncthreads();
   }
-  for (int u = tid; u < a.nb; u += 1024) {
+  for (int u0 = 0; u0 < a.nb; u0 += 1024) {
+    const int n = min(a.nb - u0, 1024), runs = min(1024 / n, nd), run = tid / n, u = u0 + tid % n;
     float x = 0.0f;
-    for (int d = 0; d < nd; ++d) x += a.buckets[d] == u ? sum[d] : 0.0f;
-    dbias[(size_t)h * a.nb + u] = (__bf16)x;
+    if (run < runs) {
+#pragma unroll 4
+      for (int d = run; d < nd; d += runs) x += bucket[d] == u ? sum[d] : 0.0f;
+    }
+    part[tid] = x;
+    __syncthreads();
+    if (tid < n) {
+      x = 0.0f;
+      for (int i = 0; i < runs; ++i) x += part[i * n + tid];
+      dbias[(size_t)h * a.nb + u] = (__bf16)x;
+    }
+    __syncthreads();
   }
 }
 

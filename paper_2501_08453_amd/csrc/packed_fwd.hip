@@ -130,14 +130,6 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void packed_fwd_kernel(PackedArgs 
   if (chunk > 0 && kt0 >= kt1) return;  // the merge does not look at it
   const int wt = (wave_keys + kBN - 1) / kBN;  // the wave's tiles: below this
 
-  bf16x8 qf[D / 16];
-  {
-    const __bf16* qp = a.q + (size_t)query_row(a, sr, qi) * a.q_tok + h * D + 8 * hi;
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const bf16x8*)(qp + 16 * ks);
-  }
-  if (BIAS) load_bias_table(a, h0, tb, tid, 64 * NW);
-
   // This wave's j-th copies of tile kt's K and V rows into ring slot `slot` (rows past nk repeat row
   // nk - 1: such keys are masked, such values zeroed before use).
   const SwzCopy<D, false> kc(a.k_tok, lane);
@@ -154,6 +146,22 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void packed_fwd_kernel(PackedArgs 
     copy16_to_lds_opaque(vbase + (size_t)first * a.v_tok, vc.offset(first, sr.nk, a.v_tok),
                          (VC_LDS char*)smem + (2 + slot) * KT + idx * Rows::GS);
   };
+  if (kt0 < kt1) {  // the first copies, in flight with the loads below
+#pragma unroll
+    for (int j = 0; j < CPW; ++j) {
+      k_copy(j, kt0, 0);
+      v_copy(j, kt0, 0);
+      k_copy(j, min(kt0 + 1, kt1 - 1), 1);
+    }
+  }
+  bf16x8 qf[D / 16];
+  {
+    const __bf16* qp = a.q + (size_t)query_row(a, sr, qi) * a.q_tok + h * D + 8 * hi;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const bf16x8*)(qp + 16 * ks);
+  }
+  if (BIAS) load_bias_table(a, h0, tb, tid, 64 * NW);
+
   const int krow = Reads::row_base(l32, hi), vtr = Reads::tr_base(lane);
   const int pos0 = w0 + sr.off;  // position of the wave's first query (with a bias: pack = 1)
 
@@ -233,12 +241,6 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void packed_fwd_kernel(PackedArgs 
 
   if (kt0 < kt1) {
     int par = 0;  // ring slot of the tile before `nxt`
-#pragma unroll
-    for (int j = 0; j < CPW; ++j) {
-      k_copy(j, kt0, 0);
-      v_copy(j, kt0, 0);
-      k_copy(j, min(kt0 + 1, kt1 - 1), 1);
-    }
     wait_all_memory();
     __syncthreads();
     if (kt0 < wt) {
