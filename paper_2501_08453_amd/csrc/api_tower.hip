@@ -90,25 +90,67 @@ vcja::PackedArgs packed_args(const vc_packedattn_desc* d, const void* q, const v
   return a;
 }
 
-// Forward: heads of a group packed into a row block, workgroups of four or eight waves, and the
-// chunks of a row block's key tiles.
+// Forward: heads of a group packed into a row block, and the chunks of a row block's key tiles.
 struct FwdPlan {
   int pack, chunks, span;
-  bool small;
+  bool few;
 };
+// The chunks of least estimated time, in tiles of 64 keys x 128 rows (about 1.8 us at head_dim 128, half
+// of that at 64, with two workgroups a compute unit): rounds over 512 places, each workgroup 3 tiles
+// more than its keys for its start and its partial results, and the merge, a launch of about 6 us and
+// the partials' way to memory and back. `share`: mean over longest keys of a block. Measured, us at 1, 2, 4, 8, 16 chunks (32 heads, 8 key heads, D = 128): 512 queries behind 16,384
+// keys -, -, 144, 157, 181; 128 behind 16,384 -, -, -, -, 57 (74 at 32); 4 x 64 behind 500 to 9,000 -, -, 62, 46,
+// 57; 8,192 causal at 4 heads 134, 113, 110, 107; two texts of 12 heads at D = 64 41, 48, 45 (3), 51 (5).
+int fwd_chunks(const vc_packedattn_desc* d, int64_t blocks, double rows, double share) {
+  const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
+  const double tile_us = d->head_dim == 128 ? 1.8 : 0.9;
+  double least = 1e30;
+  int best = 1;
+  for (int c = 1; c <= std::min(64, std::max(1, ntile / 4)); ++c) {
+    const double span = (ntile + c - 1) / c;
+    const double rounds = ceil(blocks * share * c / 512);
+    const double merge = c == 1 ? 0 : (6 + rows * c * (d->head_dim + 2) * 8 / 4e6) / tile_us;
+    const double time = rounds * (span + 3) + merge;
+    if (time < least * 0.98) {
+      least = time;
+      best = c;
+    }
+  }
+  return best;
+}
+// The same for the few-row kernel, in ns: a workgroup streams about 60 bytes a ns by itself, all of them
+// 5,200 together.
+int few_chunks(const vc_packedattn_desc* d, int64_t rows) {
+  const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
+  const double tile = 2.0 * 2 * vcja::kTileTok * d->head_dim;
+  const double all = 2.0 * 2 * d->total_k * d->kv_heads * d->head_dim / 5200;
+  double least = 1e30;
+  int best = 1;
+  for (int c = 1; c <= std::min(64, std::max(1, ntile / 2)); c += c < 8 ? 1 : c / 4) {
+    const double span = (ntile + c - 1) / c * tile;
+    const double merge = c == 1 ? 0 : 6000 + rows * c * (d->head_dim + 2) * 8 / 4000.0;
+    const double time = std::max(all + span / 120, span / 60 + 3000) + merge;
+    if (time < least * 0.98) {
+      least = time;
+      best = c;
+    }
+  }
+  return best;
+}
 FwdPlan fwd_plan(const vc_packedattn_desc* d) {
   const int group = d->heads / d->kv_heads;
   FwdPlan p;
   p.pack = !d->num_buckets && (int64_t)d->max_q * group <= 128 ? group : 1;
-  const int64_t rows = (int64_t)d->max_q * p.pack;
-  p.small = rows <= 2048;
-  const int bm = p.small ? 128 : 256;
+  const int64_t rows = (int64_t)d->max_q * p.pack, bm = vcja::kPackedRows;
   const int64_t blocks = std::min<int64_t>(d->sequences * ((rows + bm - 1) / bm), d->total_q * p.pack / bm + d->sequences) *
                          (d->heads / p.pack);
+  double share = std::min(1.0, (double)d->total_k / ((double)d->sequences * d->max_k));
+  if (d->causal && 2 * (int64_t)d->max_q > d->max_k) share *= 0.5;
+  p.few = rows <= 32;
+  const int64_t grid = d->sequences * ((rows + bm - 1) / bm) * (d->heads / p.pack), outs = d->total_q * d->heads;
   const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
-  const int64_t want = blocks >= 512 ? 1 : (1024 + blocks - 1) / blocks;
-  const int64_t grid = d->sequences * ((rows + bm - 1) / bm) * (d->heads / p.pack);
-  p.chunks = (int)std::max<int64_t>(1, std::min({want, (int64_t)ntile / 8, kMaxGrid / grid}));
+  p.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(p.few ? few_chunks(d, outs) : fwd_chunks(d, blocks, (double)outs, share),
+                                                          kMaxGrid / grid));
   p.span = (ntile + p.chunks - 1) / p.chunks;
   p.chunks = (ntile + p.span - 1) / p.span;
   return p;
@@ -122,20 +164,23 @@ size_t fwd_part_bytes(const vc_packedattn_desc* d) {
 size_t stat_bytes(const vc_packedattn_desc* d) {
   return align256((size_t)d->heads * vcja::packed_rows(d->total_q, d->sequences) * sizeof(float));
 }
-// Backward: workgroups of four waves (128 rows) or eight, and the chunks of a key block's query tiles.
-bool small_blocks(const vc_packedattn_desc* d) { return std::max(d->max_q, d->max_k) <= 2048; }
+// Backward: the chunks of a key block's query tiles (over all heads of the group). About 512
+// workgroups fill the chip twice; up to 1,024 even out the causal rule's unequal blocks where each
+// then still has 96 tiles of 32 queries to pay for its partial sums. Measured, forward and backward at D = 128,
+// us with 512 / 1,024: 4 x 1,024 tokens, 16 heads, 4 key heads 132 / 162; 16 x 1,024 394 / 432; 1 x 2,048 158 /
+// 183; 4 x 4,096 1255 / 1189; 1 x 12,000, 2 key heads 2565 / 2387.
 int key_chunks(const vc_packedattn_desc* d) {
   if (d->num_buckets) return d->heads / d->kv_heads;
-  const int bm = small_blocks(d) ? 128 : 256, group = d->heads / d->kv_heads;
-  const int64_t blocks = std::min<int64_t>((int64_t)d->sequences * ((d->max_k + bm - 1) / bm), d->total_k / bm + d->sequences);
-  const int64_t want = (1024 + d->kv_heads * blocks - 1) / (d->kv_heads * blocks);
-  const int64_t steps = (int64_t)group * ((d->max_q + 31) / 32);
+  const int bm = vcja::kPackedRows;
+  const int64_t items = d->kv_heads * std::min<int64_t>((int64_t)d->sequences * ((d->max_k + bm - 1) / bm), d->total_k / bm + d->sequences);
+  const int64_t steps = (int64_t)(d->heads / d->kv_heads) * ((d->max_q + 31) / 32);
+  const int64_t want = std::min((1024 + items - 1) / items, std::max((512 + items - 1) / items, steps / 96));
   const int64_t grid = (int64_t)d->sequences * ((d->max_k + bm - 1) / bm) * d->kv_heads;
   return (int)std::max<int64_t>(1, std::min({want, steps / 8, kMaxGrid / grid}));
 }
 size_t dist_bytes(const vc_packedattn_desc* d) {
   if (!d->num_buckets) return 0;
-  const int bm = small_blocks(d) ? 128 : 256;
+  const int bm = vcja::kPackedRows;
   return align256((size_t)(vcja::dist_row(d->total_k, d->sequences, 0, bm) + 1) * d->heads * (2 * d->max_distance + 1) * sizeof(float));
 }
 size_t key_part_bytes(const vc_packedattn_desc* d) {
@@ -183,9 +228,9 @@ vc_status vc_packedattn_fwd(const vc_packedattn_desc* desc, const void* q, const
   a.lse = lse;
   const FwdPlan p = fwd_plan(desc);
   a.pack = p.pack;
+  a.few = p.few;
   a.chunks = p.chunks;
   a.span = p.span;
-  a.small = p.small;
   a.part = static_cast<float*>(workspace);
   return vcja::launch_packed_fwd(a, desc->head_dim, as_stream(stream)) == hipSuccess ? VC_OK : VC_ERR_HIP;
 }
@@ -220,7 +265,6 @@ vc_status vc_packedattn_bwd(const vc_packedattn_desc* desc, const void* q, const
   a.dd = reinterpret_cast<float*>(ws + stat_bytes(desc));
   a.dist_part = reinterpret_cast<float*>(ws + 2 * stat_bytes(desc));
   a.key_part = reinterpret_cast<float*>(ws + 2 * stat_bytes(desc) + dist_bytes(desc));
-  a.small = small_blocks(desc);
   a.chunks = key_chunks(desc);
   return vcja::launch_packed_bwd(a, desc->head_dim, static_cast<__bf16*>(dbias), as_stream(stream)) == hipSuccess ? VC_OK
                                                                                                             : VC_ERR_HIP;

@@ -5,6 +5,8 @@
 
 namespace vcja {
 
+constexpr int kPackedWaves = 4;                  // of a workgroup
+constexpr int kPackedRows = 32 * kPackedWaves;   // query rows (keys) that it owns
 constexpr int kMaxBiasDistance = 512;  // largest relative distance with a bucket of its own
 constexpr int kMaxBuckets = 1024;
 constexpr float kBiasLimit = 65536.0f;  // bias entries below -this shut their pairs out
@@ -27,10 +29,10 @@ struct PackedArgs {
   unsigned q_tok, k_tok, v_tok;  // elements between the rows of consecutive tokens
   int causal, clear;
   float scale, scale_log2;  // softmax scale; times log2(e)
-  int nblk, bm;             // row blocks of the longest slot, rows of one
-  bool small;               // workgroups of four waves instead of eight
+  int nblk;                 // row blocks of the longest slot
   int chunks;               // workgroups that share a row block's key tiles (backward: a key block's query tiles)
   int pack, span;           // forward: heads of a group in one row block; key tiles of a chunk
+  bool few;                 // forward: all rows of a (sequence, key head) in one wave's 32
   float* part;              // forward: the chunks' partial results (see write_partial)
   float* key_part;          // their partial dK, dV: [chunks][2][Tk, Hkv, D]
   // Backward: per query row -LSE / c (-inf on padding) and -D, [H, npad], sequence s from row

@@ -1,18 +1,16 @@
 // Backward packed attention for gfx950 (see packed_fwd.hip for the layout of the sequences).
 //
-// dQ (query-stationary, first): one workgroup of eight waves owns 256 query rows of one
+// dQ (query-stationary, first): one workgroup of four waves owns 128 query rows of one
 //   (sequence, head), each wave 32, with Q^T and dO^T of its queries in registers. It forms
 //   D_i = <dO_i, O_i> from its own rows and walks over the key tiles like the forward, computing
 //   S^T, dP^T and dS^T = P^T o (dP^T - D), and dQ^T += K^T dS^T. It leaves -LSE / c and -D for the
 //   other pass.
-// dK/dV (key-stationary): one workgroup owns 256 keys of one (sequence, key head), each wave 32,
+// dK/dV (key-stationary): one workgroup owns 128 keys of one (sequence, key head), each wave 32,
 //   K and V of its keys in registers, and walks over the query tiles of 32 of every query head
 //   of the group, so that dK and dV of the shared head are summed in registers; where that leaves
 //   too few workgroups, each takes a run of those tiles and fp32 partials are summed afterwards.
 //   With a bias it also sums dS over every distance (see distance_sums).
 // No atomics anywhere: results are bitwise reproducible.
-#include <type_traits>
-
 #include "packed.hpp"
 
 namespace vcja {
@@ -69,11 +67,11 @@ __device__ __forceinline__ void clear_rows(__bf16* x, __bf16* y, const int32_t* 
   }
 }
 
-template <int D, int NW, bool BIAS>
-__global__ __launch_bounds__(64 * NW, 8 / NW) void packed_dq_kernel(PackedArgs a) {
+template <int D, bool BIAS>
+__global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedArgs a) {
   using Rows = SwzRows<D>;
   using Reads = SwzReads<D>;
-  constexpr int BM = 32 * NW;
+  constexpr int NW = kPackedWaves, BM = kPackedRows;
   constexpr int RT = Rows::bytes(kBN);
   constexpr int STAGE = 2 * RT;                  // K | V rows of a tile
   constexpr int CPW = kBN / Rows::RPC / NW;      // copies of each per wave
@@ -309,11 +307,11 @@ __device__ __forceinline__ KeySteps key_steps(const PackedArgs& a, const SeqRows
   return k;
 }
 
-template <int D, int NW, bool BIAS>
-__global__ __launch_bounds__(64 * NW, 8 / NW) void packed_dkdv_kernel(PackedArgs a) {
+template <int D, bool BIAS>
+__global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dkdv_kernel(PackedArgs a) {
   using Rows = SwzRows<D>;
   using Reads = SwzReads<D>;
-  constexpr int BM = 32 * NW;
+  constexpr int NW = kPackedWaves, BM = kPackedRows;
   constexpr int RT = Rows::bytes(kBQ);
   constexpr int STAGE = 2 * RT;               // Q rows | dO rows of a tile
   constexpr int COPIES = kBQ / Rows::RPC;     // wave copies of each
@@ -408,6 +406,7 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void packed_dkdv_kernel(PackedArgs
     load_bias_table(a, kv * a.G + g, tb, tid, 64 * NW);
     for (int i = tid; i < NW * HIST; i += 64 * NW) hist[i] = 0.0f;
     for (int i = tid; i < NW * 128; i += 64 * NW) ends[i] = 0.0f;
+    __syncthreads();  // also where no step follows
   }
   wait_all_memory();  // the loads above too: no later wait stands among copies
 
@@ -653,8 +652,8 @@ __global__ __launch_bounds__(1024) void packed_dbias_kernel(PackedArgs a, __bf16
   __shared__ int bucket[2 * kMaxBiasDistance + 1];
   const int h = blockIdx.x, nd = 2 * a.R + 1, tid = threadIdx.x;
   for (int d = tid; d < nd; d += 1024) bucket[d] = a.buckets[d];
-  const int r0 = (int)dist_row(min(max(a.cu_k[0], 0), a.Tk), 0, 0, a.bm);
-  const int r1 = (int)dist_row(min(max(a.cu_k[a.S], 0), a.Tk), a.S, 0, a.bm);
+  const int r0 = (int)dist_row(min(max(a.cu_k[0], 0), a.Tk), 0, 0, kPackedRows);
+  const int r1 = (int)dist_row(min(max(a.cu_k[a.S], 0), a.Tk), a.S, 0, kPackedRows);
   const float* rows = a.dist_part + (size_t)h * nd;
   const size_t one = (size_t)a.H * nd;
   for (int d0 = 0; d0 < nd; d0 += 1024) {
@@ -694,15 +693,13 @@ __global__ __launch_bounds__(1024) void packed_dbias_kernel(PackedArgs a, __bf16
 }  // namespace
 
 namespace {
-template <int D, int NW, bool BIAS>
+template <int D, bool BIAS>
 void launch_bwd(PackedArgs a, __bf16* dbias, int clear, hipStream_t s) {
-  constexpr int BM = 32 * NW;
-  const dim3 block(64 * NW);
-  a.bm = BM;
-  a.nblk = (a.max_q + BM - 1) / BM;
-  hipLaunchKernelGGL((packed_dq_kernel<D, NW, BIAS>), dim3(a.nblk * a.H * a.S + clear), block, 0, s, a);
-  a.nblk = (a.max_k + BM - 1) / BM;
-  hipLaunchKernelGGL((packed_dkdv_kernel<D, NW, BIAS>), dim3(a.nblk * a.Hkv * a.S * a.chunks + clear), block, 0, s, a);
+  const dim3 block(64 * kPackedWaves);
+  a.nblk = (a.max_q + kPackedRows - 1) / kPackedRows;
+  hipLaunchKernelGGL((packed_dq_kernel<D, BIAS>), dim3(a.nblk * a.H * a.S + clear), block, 0, s, a);
+  a.nblk = (a.max_k + kPackedRows - 1) / kPackedRows;
+  hipLaunchKernelGGL((packed_dkdv_kernel<D, BIAS>), dim3(a.nblk * a.Hkv * a.S * a.chunks + clear), block, 0, s, a);
   if (a.chunks > 1) {
     const size_t threads = (size_t)a.Tk * a.Hkv * D / 4;
     hipLaunchKernelGGL(packed_key_sum_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, a.Hkv * D);
@@ -713,21 +710,14 @@ void launch_bwd(PackedArgs a, __bf16* dbias, int clear, hipStream_t s) {
 
 hipError_t launch_packed_bwd(const PackedArgs& a, int head_dim, __bf16* dbias, hipStream_t s) {
   const int clear = a.clear ? 32 : 0;
-  auto go = [&](auto d, auto bias) {
-    if (a.small)
-      launch_bwd<decltype(d)::value, 4, decltype(bias)::value>(a, dbias, clear, s);
-    else
-      launch_bwd<decltype(d)::value, 8, decltype(bias)::value>(a, dbias, clear, s);
-  };
-  using std::integral_constant;
   if (head_dim == 128 && a.bias)
-    go(integral_constant<int, 128>{}, std::true_type{});
+    launch_bwd<128, true>(a, dbias, clear, s);
   else if (head_dim == 128)
-    go(integral_constant<int, 128>{}, std::false_type{});
+    launch_bwd<128, false>(a, dbias, clear, s);
   else if (a.bias)
-    go(integral_constant<int, 64>{}, std::true_type{});
+    launch_bwd<64, true>(a, dbias, clear, s);
   else
-    go(integral_constant<int, 64>{}, std::false_type{});
+    launch_bwd<64, false>(a, dbias, clear, s);
   return hipGetLastError();
 }
 

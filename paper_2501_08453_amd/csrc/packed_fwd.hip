@@ -1,24 +1,24 @@
 // Forward packed attention for gfx950: sequences of different lengths laid one behind the
 // other, grouped heads, causal or not, with an optional bias per bucket of the distance.
 //
-// One workgroup of four or eight waves owns 128 or 256 query rows of one (sequence, head), each
-// wave 32 held in registers; keys and values stream through LDS in tiles of 64 as in the joint
-// forward. The wave computes S^T = K Q^T, so that a lane's accumulator column is one query, and
+// One workgroup of four waves owns 128 query rows of one (sequence, head), each wave 32 held in
+// registers; two workgroups share a compute unit. (Eight waves and 256 rows, as in the joint forward,
+// are 1% faster at 8,192 tokens and up and up to twice as slow below: 509 -> 504 us there, 48 -> 90 us
+// at 2,048, both at 32 heads, D = 128.) Keys and values stream through LDS in tiles of 64. The wave computes S^T = K Q^T, so that a lane's accumulator column is one query, and
 // O^T += V^T P^T with P^T straight from the accumulator layout. Software pipeline: at step j the
 // matrix cores get the scores of tile j+1 and then O += P_j V_j, and the softmax of tile j+1
 // runs on the vector ALUs among the latter. The exponent base is raised only when a lane's sum
 // of 32 probabilities against it exceeds 2^13 (see the joint forward). Probabilities are summed
 // unrounded, so that LSE holds to fp32; they are rounded to bf16 for the product with V, the
 // matrix cores' operand type. Under the causal rule each wave stops at its own last tile.
-#include <algorithm>
-#include <type_traits>
-
 #include "packed.hpp"
 
 namespace vcja {
 namespace {
 
 constexpr int kBN = kTileTok;
+constexpr int kFewWaves = 4;          // of a workgroup of the few-row kernel
+constexpr int few_tile(int d) { return d == 128 ? 32 : 64; }  // keys of one of its tiles
 constexpr float kSumLimit = 8192.0f;  // largest accepted sum of a lane's 32 probabilities
 
 // Probabilities 2^(s c log2(e) + sub) of 8 scores (one PV operand), rounded to bf16, with their
@@ -56,6 +56,15 @@ __device__ __forceinline__ float raise_base(const f32x16* s, float scale_log2, f
   return alpha;
 }
 
+// Waits until at most N vector-memory operations of this wave are in flight (they end in order).
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// Waits for this wave's LDS operations.
+__device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // O = 0 and LSE = -inf for the rows outside every slot (the last workgroups of a grid).
 template <int D>
 __device__ __forceinline__ void clear_o(const PackedArgs& a, int wg, int wgs, int tid, int threads) {
@@ -90,11 +99,11 @@ __device__ __forceinline__ void write_partial(const PackedArgs& a, int chunk, in
 
 // The query rows of a workgroup: row r is query r / pack, head r % pack of its block of heads
 // (pack = 1: one head; pack = the group: its heads share every tile of keys).
-template <int D, int NW, bool BIAS>
-__global__ __launch_bounds__(64 * NW, 8 / NW) void packed_fwd_kernel(PackedArgs a) {
+template <int D, bool BIAS>
+__global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_fwd_kernel(PackedArgs a) {
   using Rows = SwzRows<D>;
   using Reads = SwzReads<D>;
-  constexpr int BM = 32 * NW;
+  constexpr int NW = kPackedWaves, BM = kPackedRows;
   constexpr int KT = Rows::bytes(kBN);
   constexpr int CPW = kBN / Rows::RPC / NW;  // copies of a K (V) tile per wave
   __shared__ __attribute__((aligned(1024))) char smem[4 * KT];  // K ring | V ring
@@ -352,81 +361,264 @@ __global__ __launch_bounds__(64 * NW, 8 / NW) void packed_fwd_kernel(PackedArgs 
     a.lse[(size_t)h * a.Tq + sr.q0 + qi] = lt == 0.0f ? -INFINITY : (m + __log2f(lt)) * kLn2;
 }
 
-// O and LSE of the rows whose keys several workgroups share, from their partials in order:
-// O = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l_c over the chunks that hold keys (M the largest of
-// their bases). One thread per 4 dims of one (query, head).
-template <int D>
-__global__ __launch_bounds__(256) void packed_merge_kernel(PackedArgs a, int rows_per_block) {
-  const int64_t x = ((int64_t)blockIdx.x * 256 + threadIdx.x) / (D / 4);
-  const int d = (int)(threadIdx.x % (D / 4)) * 4;
-  if (x >= (int64_t)a.S * a.max_q * a.H) return;
-  const int h = (int)(x % a.H), i = (int)(x / a.H % a.max_q), s = (int)(x / a.H / a.max_q);
-  const int q0 = min(max(a.cu_q[s], 0), a.Tq), sq = min(min(max(a.cu_q[s + 1], q0), a.Tq) - q0, a.max_q);
-  if (i >= sq) return;
-  const int nq = a.len_q ? min(max(a.len_q[s], 0), sq) : sq;
-  const int k0 = min(max(a.cu_k[s], 0), a.Tk), sk = min(min(max(a.cu_k[s + 1], k0), a.Tk) - k0, a.max_k);
-  const int nk = a.len_k ? min(max(a.len_k[s], 0), sk) : sk;
-  // The tiles of the row's block of rows, as the forward counts them.
-  const int row = i * a.pack + h % a.pack, b0 = row / rows_per_block * rows_per_block;
-  const int last = (min(b0 + rows_per_block, nq * a.pack) - 1) / a.pack;
-  const int keys = b0 >= nq * a.pack ? 0 : a.causal ? max(0, min(nk, last + nk - nq + 1)) : nk;
-  const int n = ((keys + kBN - 1) / kBN + a.span - 1) / a.span;
-  if (n <= 1) return;  // written by its only workgroup
-  const size_t rows = (size_t)a.Tq * a.H, at = (size_t)(q0 + i) * a.H + h;
-  const float* ml = a.part + (size_t)a.chunks * rows * D;
-  float mx = -INFINITY;
-#pragma unroll 4
-  for (int c = 0; c < n; ++c) {
-    const float* p = ml + (c * rows + at) * 2;
-    mx = fmaxf(mx, p[1] > 0.0f ? p[0] : -INFINITY);
+// Few rows (single tokens or a few drafted ones at the end of a cache; rows of all heads of a group
+// together, 32 at most): memory-bound, so the waves of a workgroup share the keys, not the
+// rows. Each wave streams every NW-th tile of its chunk (8 KiB of keys and 8 KiB of values) through
+// a ring of its own, waiting for one tile while the next is in flight, without a barrier; the
+// waves' results are joined in LDS at the end.
+template <int D, bool BIAS>
+__global__ __launch_bounds__(64 * kFewWaves) void packed_few_kernel(PackedArgs a) {
+  using Rows = SwzRows<D>;
+  using Reads = SwzReads<D>;
+  constexpr int NW = kFewWaves, KBT = few_tile(D), KB = KBT / 32;
+  constexpr int KT = Rows::bytes(KBT);
+  constexpr int COPIES = KBT / Rows::RPC;
+  constexpr int RING = 4 * KT;       // of a wave: two stages of K | V
+  constexpr int OS = D + 4;          // floats between the rows of a wave's O
+  static_assert(RING >= 32 * OS * 4, "O of a wave fits its ring");
+  __shared__ __attribute__((aligned(1024))) char smem[NW * RING];
+  __shared__ float ml[NW][32][2];
+  __shared__ float tb[BIAS ? kBiasTable : 1];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, hi = lane >> 5;
+  const int heads = a.H / a.pack, items = heads * a.S * a.chunks;
+  if ((int)blockIdx.x >= items) {
+    clear_o<D>(a, blockIdx.x - items, gridDim.x - items, tid, 64 * NW);
+    return;
   }
-  float sum = 0.0f;
-  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-  for (int c = 0; c < n; ++c) {
-    const float* p = ml + (c * rows + at) * 2;
-    const f32x4 o = *(const f32x4*)(a.part + (c * rows + at) * D + d);
-    const float l = p[1], wgt = l == 0.0f ? 0.0f : exp2f(p[0] - mx);
-    sum += wgt * l;
+  const int hb = blockIdx.x % heads, s = blockIdx.x / heads % a.S, chunk = blockIdx.x / heads / a.S;
+  const SeqRows sr = seq_rows(a, s);
+  if (sr.sq == 0) return;
+  const int h0 = hb * a.pack, kv = h0 / a.G;
+  const int qi = a.pack == 1 ? l32 : l32 / a.pack, h = h0 + l32 - qi * a.pack;
+  auto limit = [&](int i) { return a.causal ? max(0, min(sr.nk, i + sr.off + 1)) : sr.nk; };
+  const int keys = sr.nq > 0 ? limit(sr.nq - 1) : 0, all = limit(0);
+  const int klim = qi < sr.nq ? limit(qi) : 0;
+  // This workgroup's tiles, of `few_tile` keys; the span counts tiles of 64.
+  const int k_begin = chunk * a.span * kBN, k_end = min(keys, k_begin + a.span * kBN);
+  if (chunk > 0 && k_begin >= k_end) return;  // the merge does not look at it
+  const int t_end = (k_end + KBT - 1) / KBT;
+
+  const SwzCopy<D, false> kc(a.k_tok, lane);
+  const SwzCopy<D, true> vc(a.v_tok, lane);
+  const __bf16* kbase = a.k + (size_t)sr.k0 * a.k_tok + kv * D;
+  const __bf16* vbase = a.v + (size_t)sr.k0 * a.v_tok + kv * D;
+  VC_LDS char* ring = (VC_LDS char*)smem + w * RING;
+  auto copy_tile = [&](int t, int st) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] += l == 0.0f ? 0.0f : wgt * o[e];
+    for (int j = 0; j < COPIES; ++j) {
+      const int fk = swz_copy_row<D, false>(t * KBT, sr.nk, j), fv = swz_copy_row<D, true>(t * KBT, sr.nk, j);
+      copy16_to_lds_opaque(kbase + (size_t)fk * a.k_tok, kc.offset(fk, sr.nk, a.k_tok), ring + st * 2 * KT + j * Rows::GS);
+      copy16_to_lds_opaque(vbase + (size_t)fv * a.v_tok, vc.offset(fv, sr.nk, a.v_tok), ring + (st * 2 + 1) * KT + j * Rows::GS);
+    }
+  };
+  int t = k_begin / KBT + w;
+  if (t < t_end) copy_tile(t, 0);
+  bf16x8 qf[D / 16];
+  {
+    const __bf16* qp = a.q + (size_t)query_row(a, sr, qi) * a.q_tok + h * D + 8 * hi;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const bf16x8*)(qp + 16 * ks);
   }
-  const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
-  *(bf16x4*)(a.o + at * D + d) = bf16x4{(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv),
-                                        (__bf16)(acc[3] * inv)};
-  if (d == 0) a.lse[(size_t)h * a.Tq + q0 + i] = sum == 0.0f ? -INFINITY : (mx + log2f(sum)) * kLn2;
+  if (BIAS) {
+    load_bias_table(a, h0, tb, tid, 64 * NW);
+    __syncthreads();
+  }
+  wait_all_memory();
+
+  f32x16 oacc[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) oacc[i] = zero_f32x16();
+  float m = -INFINITY, l = 0.0f;
+  const int krow = Reads::row_base(l32, hi), vtr = Reads::tr_base(lane);
+  for (int st = 0; t < t_end; t += NW, st ^= 1) {
+    if (t + NW < t_end) {
+      wait_reads();  // of the tile before: its stage is written again
+      copy_tile(t + NW, st ^ 1);
+      wait_loads<2 * COPIES>();  // all but the copies just issued
+    } else {
+      wait_loads<0>();
+    }
+    const int k0 = t * KBT;
+    const VC_LDS char* kp = ring + st * 2 * KT + krow;
+    const VC_LDS char* vp = ring + (st * 2 + 1) * KT + vtr;
+    if (k0 + KBT > sr.nk) {  // value rows past nk: zero (0 * inf is not)
+#pragma unroll
+      for (int j = 0; j < COPIES; ++j)
+        if (k0 + perm_row(Rows::RPC * j + lane / Rows::CPR) >= sr.nk)
+          *(VC_LDS bf16x8*)(ring + (st * 2 + 1) * KT + j * Rows::GS + 16 * lane) = zero_bf16x8();
+    }
+    f32x16 sc[KB];
+    float shift = 0.0f;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) sc[kb] = zero_f32x16();
+    if (BIAS) {
+      const int side = bias_side(k0, k0 + KBT - 1, sr.off, sr.off + 31, a.R);
+      if (side == 0) {
+        const float* b = tb + kBiasPad + a.R + (k0 + 4 * hi - sr.off - l32);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sc[kb][r] = b[kb * 32 + 8 * (r >> 2) + (r & 3)];
+      } else {
+        shift = tb[kBiasPad + (side > 0 ? 2 * a.R : 0)] * a.scale_log2;
+      }
+    }
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+        sc[kb] = mfma32(*(const VC_LDS bf16x8*)(Reads::row_at(kp, ks) + kb * Rows::bytes(32)), qf[ks], sc[kb]);
+    if (k0 + KBT > all || l32 >= sr.nq * a.pack) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[kb][r] = k0 + kb * 32 + acc_row(r, hi) < klim ? sc[kb][r] : -INFINITY;
+    }
+    bf16x8 pb[2 * KB];
+    float psum = 0.0f, alpha = 1.0f;
+    const float sub = shift - m;
+#pragma unroll
+    for (int c = 0; c < 2 * KB; ++c) pb[c] = probs8(sc[c >> 1], c & 1, a.scale_log2, sub, psum);
+    const bool need = !(psum <= kSumLimit);
+    if (__any(need)) {
+      alpha = raise_base<KB>(sc, a.scale_log2, shift, need, m, pb, psum);
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) oacc[i] *= alpha;
+    }
+    l = fmaf(l, alpha, psum);
+#pragma unroll
+    for (int c = 0; c < 2 * KB; ++c)
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) oacc[db] = mfma32(Reads::tr_operand(vp, c, db), pb[c], oacc[db]);
+  }
+  // The waves' results, joined in order: O = sum_w 2^(m_w - M) O_w, l likewise.
+  l = halves_sum(l);
+  wait_all_memory();
+  VC_LDS float* ow = (VC_LDS float*)ring + l32 * OS;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *(VC_LDS f32x4*)(ow + db * 32 + 8 * j + 4 * hi) =
+          f32x4{oacc[db][4 * j + 0], oacc[db][4 * j + 1], oacc[db][4 * j + 2], oacc[db][4 * j + 3]};
+  if (hi == 0) {
+    ml[w][l32][0] = m;
+    ml[w][l32][1] = l;
+  }
+  __syncthreads();
+  const bool split = (keys + kBN - 1) / kBN > a.span;
+  for (int i = tid; i < sr.sq * a.pack * (D / 4); i += 64 * NW) {
+    const int r = i / (D / 4), d = i % (D / 4) * 4;
+    const int q = r / a.pack, head = h0 + r % a.pack;
+    float mx = -INFINITY, sum = 0.0f;
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < NW; ++j) mx = fmaxf(mx, ml[j][r][1] == 0.0f ? -INFINITY : ml[j][r][0]);
+#pragma unroll
+    for (int j = 0; j < NW; ++j) {
+      const float lj = ml[j][r][1], wgt = lj == 0.0f ? 0.0f : fast_exp2(ml[j][r][0] - mx);
+      const f32x4 x = *(const VC_LDS f32x4*)((const VC_LDS float*)((VC_LDS char*)smem + j * RING) + r * OS + d);
+      sum += wgt * lj;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += lj == 0.0f ? 0.0f : wgt * x[e];
+    }
+    const size_t rows = (size_t)a.Tq * a.H, at = (size_t)(sr.q0 + q) * a.H + head;
+    if (split) {
+      *(f32x4*)(a.part + (chunk * rows + at) * D + d) = o;
+      if (d == 0) {
+        float* p = a.part + (size_t)a.chunks * rows * D + (chunk * rows + at) * 2;
+        p[0] = mx;
+        p[1] = sum;
+      }
+    } else {
+      const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
+      *(bf16x4*)(a.o + at * D + d) = bf16x4{(__bf16)(o[0] * inv), (__bf16)(o[1] * inv), (__bf16)(o[2] * inv), (__bf16)(o[3] * inv)};
+      if (d == 0) a.lse[(size_t)head * a.Tq + sr.q0 + q] = sum == 0.0f ? -INFINITY : (mx + __log2f(sum)) * kLn2;
+    }
+  }
 }
 
-template <int D, int NW, bool BIAS>
-void launch_blocks(PackedArgs a, int clear, hipStream_t s) {
-  constexpr int BM = 32 * NW;
-  a.nblk = (a.max_q * a.pack + BM - 1) / BM;
-  hipLaunchKernelGGL((packed_fwd_kernel<D, NW, BIAS>), dim3(a.nblk * (a.H / a.pack) * a.S * a.chunks + clear), dim3(64 * NW), 0, s, a);
-  if (a.chunks > 1) {
-    const int64_t threads = (int64_t)a.S * a.max_q * a.H * (D / 4);
-    hipLaunchKernelGGL(packed_merge_kernel<D>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, BM);
+__device__ __forceinline__ float lane_value(float x, int lane) {  // lane < 64, the same for the wave
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+}
+
+// O and LSE of the rows whose keys several workgroups share, from their partials in order:
+// O = sum_c 2^(m_c - M) O_c / sum_c 2^(m_c - M) l_c over the chunks that hold keys (M the largest of
+// their bases). One wave per (query, head): lane c weighs chunk c, then each lane sums D / 64 dims.
+template <int D>
+__global__ __launch_bounds__(256) void packed_merge_kernel(PackedArgs a) {
+  constexpr int E = D / 64;
+  typedef float fe __attribute__((ext_vector_type(E)));
+  const int lane = threadIdx.x & 63;
+  const int x = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  if (x >= a.S * a.max_q * a.H) return;
+  const int h = x % a.H, i = x / a.H % a.max_q;
+  const SeqRows sr = seq_rows(a, x / a.H / a.max_q);
+  if (i >= sr.sq) return;
+  // The keys of the row's block of rows, as the forward counts them.
+  const int row = i * a.pack + h % a.pack, b0 = row / kPackedRows * kPackedRows;
+  const int last = (min(b0 + kPackedRows, sr.nq * a.pack) - 1) / a.pack;
+  const int keys = b0 >= sr.nq * a.pack ? 0 : a.causal ? max(0, min(sr.nk, last + sr.off + 1)) : sr.nk;
+  const int n = ((keys + kBN - 1) / kBN + a.span - 1) / a.span;
+  if (n <= 1) return;  // written by its only workgroup
+  const size_t rows = (size_t)a.Tq * a.H, at = (size_t)(sr.q0 + i) * a.H + h;
+  const float* p = a.part + (size_t)a.chunks * rows * D + (min(lane, n - 1) * rows + at) * 2;
+  const float l = lane < n ? p[1] : 0.0f, mc = l == 0.0f ? -INFINITY : p[0];
+  float mx = mc;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+  const float wgt = l == 0.0f ? 0.0f : exp2f(mc - mx);
+  float sum = wgt * l;
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  fe acc;
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+  for (int c0 = 0; c0 < n; c0 += 8) {  // eight loads in flight
+    fe o[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = *(const fe*)(a.part + (min(c0 + j, n - 1) * rows + at) * D + E * lane);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {  // lanes from n on weigh nothing
+      const float wc = lane_value(wgt, c0 + j);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += wc == 0.0f ? 0.0f : wc * o[j][e];
+    }
   }
+  const float inv = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
+  __bf16* to = a.o + at * D + E * lane;
+#pragma unroll
+  for (int e = 0; e < E; ++e) to[e] = (__bf16)(acc[e] * inv);
+  if (lane == 0) a.lse[(size_t)h * a.Tq + sr.q0 + i] = sum == 0.0f ? -INFINITY : (mx + log2f(sum)) * kLn2;
+}
+
+template <int D, bool BIAS>
+void launch(PackedArgs a, hipStream_t s) {
+  const int clear = a.clear ? 32 : 0, heads = a.H / a.pack;
+  if (a.few) {
+    hipLaunchKernelGGL((packed_few_kernel<D, BIAS>), dim3(heads * a.S * a.chunks + clear), dim3(64 * kFewWaves), 0, s, a);
+  } else {
+    a.nblk = (a.max_q * a.pack + kPackedRows - 1) / kPackedRows;
+    hipLaunchKernelGGL((packed_fwd_kernel<D, BIAS>), dim3(a.nblk * heads * a.S * a.chunks + clear), dim3(64 * kPackedWaves), 0, s, a);
+  }
+  if (a.chunks > 1) hipLaunchKernelGGL(packed_merge_kernel<D>, dim3((a.S * a.max_q * a.H + 3) / 4), dim3(256), 0, s, a);
 }
 
 }  // namespace
 
 hipError_t launch_packed_fwd(const PackedArgs& a, int head_dim, hipStream_t s) {
-  const int clear = a.clear ? 32 : 0;
-  auto go = [&](auto d, auto bias) {
-    if (a.small)
-      launch_blocks<decltype(d)::value, 4, decltype(bias)::value>(a, clear, s);
-    else
-      launch_blocks<decltype(d)::value, 8, decltype(bias)::value>(a, clear, s);
-  };
-  using std::integral_constant;
   if (head_dim == 128 && a.bias)
-    go(integral_constant<int, 128>{}, std::true_type{});
+    launch<128, true>(a, s);
   else if (head_dim == 128)
-    go(integral_constant<int, 128>{}, std::false_type{});
+    launch<128, false>(a, s);
   else if (a.bias)
-    go(integral_constant<int, 64>{}, std::true_type{});
+    launch<64, true>(a, s);
   else
-    go(integral_constant<int, 64>{}, std::false_type{});
+    launch<64, false>(a, s);
   return hipGetLastError();
 }
 

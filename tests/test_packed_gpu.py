@@ -253,6 +253,16 @@ def test_longer_sequences(nb, causal, D):
     check(*make(28, [2100, 70, 1], [2100, 300, 1], 2, 1 if nb == 0 else 2, D, causal, nb, 100 if nb else 0))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("nb", [0, 12])
+@pytest.mark.parametrize("lq,H,Hkv", [([1, 1, 1, 1, 0], 8, 2), ([4, 4, 4, 4, 4], 16, 2), ([7, 1, 3, 2, 5], 4, 4), ([33, 1, 40, 8, 2], 4, 2)])
+def test_few_rows_behind_long_caches(lq, H, Hkv, nb, D):
+    """Single and drafted tokens, the rows of a group's heads together (up to 32, and more), keys over several workgroups,
+    slots longer than what they hold (NaN behind it), in both directions."""
+    x, d, desc = make(29, lq, [9000, 64, 1, 2049, 333], H, Hkv if nb == 0 else H, D, True, nb, 60 if nb else 0, slack=(2, 70), outside=(0, 3))
+    check(x, d, desc)
+
+
 def test_reproducible():
     """Two runs agree bitwise."""
     import torch
