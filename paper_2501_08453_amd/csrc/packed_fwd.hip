@@ -364,16 +364,17 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_fwd_kernel(Packed
 // Few rows (single tokens or a few drafted ones at the end of a cache; rows of all heads of a group
 // together, 32 at most): memory-bound, so the waves of a workgroup share the keys, not the
 // rows. Each wave streams every NW-th tile of its chunk (8 KiB of keys and 8 KiB of values) through
-// a ring of its own, waiting for one tile while the next is in flight, without a barrier; the
-// waves' results are joined in LDS at the end.
+// LDS of its own without a barrier, the next tile's keys in flight once the scores are formed, its
+// values once they are used, eight waves a compute unit; their results are joined in LDS at the
+// end.
 template <int D, bool BIAS>
-__global__ __launch_bounds__(64 * kFewWaves) void packed_few_kernel(PackedArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves, 8 / kFewWaves) void packed_few_kernel(PackedArgs a) {
   using Rows = SwzRows<D>;
   using Reads = SwzReads<D>;
   constexpr int NW = kFewWaves, KBT = few_tile(D), KB = KBT / 32;
   constexpr int KT = Rows::bytes(KBT);
   constexpr int COPIES = KBT / Rows::RPC;
-  constexpr int RING = 4 * KT;       // of a wave: two stages of K | V
+  constexpr int RING = 2 * KT;       // of a wave: K | V
   constexpr int OS = D + 4;          // floats between the rows of a wave's O
   static_assert(RING >= 32 * OS * 4, "O of a wave fits its ring");
   __shared__ __attribute__((aligned(1024))) char smem[NW * RING];
@@ -407,16 +408,25 @@ __global__ __launch_bounds__(64 * kFewWaves) void packed_few_kernel(PackedArgs a
   const __bf16* kbase = a.k + (size_t)sr.k0 * a.k_tok + kv * D;
   const __bf16* vbase = a.v + (size_t)sr.k0 * a.v_tok + kv * D;
   VC_LDS char* ring = (VC_LDS char*)smem + w * RING;
-  auto copy_tile = [&](int t, int st) {
+  auto copy_k = [&](int t) {
 #pragma unroll
     for (int j = 0; j < COPIES; ++j) {
-      const int fk = swz_copy_row<D, false>(t * KBT, sr.nk, j), fv = swz_copy_row<D, true>(t * KBT, sr.nk, j);
-      copy16_to_lds_opaque(kbase + (size_t)fk * a.k_tok, kc.offset(fk, sr.nk, a.k_tok), ring + st * 2 * KT + j * Rows::GS);
-      copy16_to_lds_opaque(vbase + (size_t)fv * a.v_tok, vc.offset(fv, sr.nk, a.v_tok), ring + (st * 2 + 1) * KT + j * Rows::GS);
+      const int first = swz_copy_row<D, false>(t * KBT, sr.nk, j);
+      copy16_to_lds_opaque(kbase + (size_t)first * a.k_tok, kc.offset(first, sr.nk, a.k_tok), ring + j * Rows::GS);
+    }
+  };
+  auto copy_v = [&](int t) {
+#pragma unroll
+    for (int j = 0; j < COPIES; ++j) {
+      const int first = swz_copy_row<D, true>(t * KBT, sr.nk, j);
+      copy16_to_lds_opaque(vbase + (size_t)first * a.v_tok, vc.offset(first, sr.nk, a.v_tok), ring + KT + j * Rows::GS);
     }
   };
   int t = k_begin / KBT + w;
-  if (t < t_end) copy_tile(t, 0);
+  if (t < t_end) {
+    copy_k(t);
+    copy_v(t);
+  }
   bf16x8 qf[D / 16];
   {
     const __bf16* qp = a.q + (size_t)query_row(a, sr, qi) * a.q_tok + h * D + 8 * hi;
@@ -434,23 +444,12 @@ __global__ __launch_bounds__(64 * kFewWaves) void packed_few_kernel(PackedArgs a
   for (int i = 0; i < D / 32; ++i) oacc[i] = zero_f32x16();
   float m = -INFINITY, l = 0.0f;
   const int krow = Reads::row_base(l32, hi), vtr = Reads::tr_base(lane);
-  for (int st = 0; t < t_end; t += NW, st ^= 1) {
-    if (t + NW < t_end) {
-      wait_reads();  // of the tile before: its stage is written again
-      copy_tile(t + NW, st ^ 1);
-      wait_loads<2 * COPIES>();  // all but the copies just issued
-    } else {
-      wait_loads<0>();
-    }
+  for (; t < t_end; t += NW) {
+    const bool more = t + NW < t_end;
+    wait_loads<COPIES>();  // the tile's keys have landed; its values may be in flight
     const int k0 = t * KBT;
-    const VC_LDS char* kp = ring + st * 2 * KT + krow;
-    const VC_LDS char* vp = ring + (st * 2 + 1) * KT + vtr;
-    if (k0 + KBT > sr.nk) {  // value rows past nk: zero (0 * inf is not)
-#pragma unroll
-      for (int j = 0; j < COPIES; ++j)
-        if (k0 + perm_row(Rows::RPC * j + lane / Rows::CPR) >= sr.nk)
-          *(VC_LDS bf16x8*)(ring + (st * 2 + 1) * KT + j * Rows::GS + 16 * lane) = zero_bf16x8();
-    }
+    const VC_LDS char* kp = ring + krow;
+    const VC_LDS char* vp = ring + KT + vtr;
     f32x16 sc[KB];
     float shift = 0.0f;
 #pragma unroll
@@ -472,6 +471,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void packed_few_kernel(PackedArgs a
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
         sc[kb] = mfma32(*(const VC_LDS bf16x8*)(Reads::row_at(kp, ks) + kb * Rows::bytes(32)), qf[ks], sc[kb]);
+    if (more) {
+      wait_reads();
+      copy_k(t + NW);
+    }
     if (k0 + KBT > all || l32 >= sr.nq * a.pack) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
@@ -490,10 +493,24 @@ __global__ __launch_bounds__(64 * kFewWaves) void packed_few_kernel(PackedArgs a
       for (int i = 0; i < D / 32; ++i) oacc[i] *= alpha;
     }
     l = fmaf(l, alpha, psum);
+    if (more)
+      wait_loads<COPIES>();
+    else
+      wait_loads<0>();
+    if (k0 + KBT > sr.nk) {  // value rows past nk: zero (0 * inf is not)
+#pragma unroll
+      for (int j = 0; j < COPIES; ++j)
+        if (k0 + perm_row(Rows::RPC * j + lane / Rows::CPR) >= sr.nk)
+          *(VC_LDS bf16x8*)(ring + KT + j * Rows::GS + 16 * lane) = zero_bf16x8();
+    }
 #pragma unroll
     for (int c = 0; c < 2 * KB; ++c)
 #pragma unroll
       for (int db = 0; db < D / 32; ++db) oacc[db] = mfma32(Reads::tr_operand(vp, c, db), pb[c], oacc[db]);
+    if (more) {
+      wait_reads();
+      copy_v(t + NW);
+    }
   }
   // The waves' results, joined in order: O = sum_w 2^(m_w - M) O_w, l likewise.
   l = halves_sum(l);
