@@ -98,17 +98,18 @@ struct FwdPlan {
 // The chunks of least estimated time, in tiles of 64 keys x 128 rows (about 1.8 us at head_dim 128, half
 // of that at 64, with two workgroups a compute unit): rounds over 512 places, each workgroup 3 tiles
 // more than its keys for its start and its partial results, and the merge, a launch of about 6 us and
-// the partials' way to memory and back. `share`: mean over longest keys of a block. Measured, us at 1, 2, 4, 8, 16 chunks (32 heads, 8 key heads, D = 128): 512 queries behind 16,384
+// the partials' way to memory and back. `share`: mean over longest keys of a block; `uneven` blocks (the
+// causal rule's, longest first) fill their last round. Measured, us at 1, 2, 4, 8, 16 chunks (32 heads, 8 key heads, D = 128): 512 queries behind 16,384
 // keys -, -, 144, 157, 181; 128 behind 16,384 -, -, -, -, 57 (74 at 32); 4 x 64 behind 500 to 9,000 -, -, 62, 46,
 // 57; 8,192 causal at 4 heads 134, 113, 110, 107; two texts of 12 heads at D = 64 41, 48, 45 (3), 51 (5).
-int fwd_chunks(const vc_packedattn_desc* d, int64_t blocks, double rows, double share) {
+int fwd_chunks(const vc_packedattn_desc* d, int64_t blocks, double rows, double share, bool uneven) {
   const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
   const double tile_us = d->head_dim == 128 ? 1.8 : 0.9;
   double least = 1e30;
   int best = 1;
   for (int c = 1; c <= std::min(64, std::max(1, ntile / 4)); ++c) {
     const double span = (ntile + c - 1) / c;
-    const double rounds = ceil(blocks * share * c / 512);
+    const double load = blocks * share * c / 512, rounds = uneven ? std::max(load, 1.0) : ceil(load);
     const double merge = c == 1 ? 0 : (6 + rows * c * (d->head_dim + 2) * 8 / 4e6) / tile_us;
     const double time = rounds * (span + 3) + merge;
     if (time < least * 0.98) {
@@ -145,11 +146,12 @@ FwdPlan fwd_plan(const vc_packedattn_desc* d) {
   const int64_t blocks = std::min<int64_t>(d->sequences * ((rows + bm - 1) / bm), d->total_q * p.pack / bm + d->sequences) *
                          (d->heads / p.pack);
   double share = std::min(1.0, (double)d->total_k / ((double)d->sequences * d->max_k));
-  if (d->causal && 2 * (int64_t)d->max_q > d->max_k) share *= 0.5;
+  const bool uneven = d->causal && 2 * (int64_t)d->max_q > d->max_k;
+  if (uneven) share *= 0.5;
   p.few = rows <= 32;
   const int64_t grid = d->sequences * ((rows + bm - 1) / bm) * (d->heads / p.pack), outs = d->total_q * d->heads;
   const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
-  p.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(p.few ? few_chunks(d, outs) : fwd_chunks(d, blocks, (double)outs, share),
+  p.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(p.few ? few_chunks(d, outs) : fwd_chunks(d, blocks, (double)outs, share, uneven),
                                                           kMaxGrid / grid));
   p.span = (ntile + p.chunks - 1) / p.chunks;
   p.chunks = (ntile + p.span - 1) / p.span;
@@ -170,18 +172,20 @@ size_t stat_bytes(const vc_packedattn_desc* d) {
 // us with 512 / 1,024: 4 x 1,024 tokens, 16 heads, 4 key heads 132 / 162; 16 x 1,024 394 / 432; 1 x 2,048 158 /
 // 183; 4 x 4,096 1255 / 1189; 1 x 12,000, 2 key heads 2565 / 2387.
 int key_chunks(const vc_packedattn_desc* d) {
-  if (d->num_buckets) return d->heads / d->kv_heads;
-  const int bm = vcja::kPackedRows;
+  const int bm = vcja::kPackedRows, group = d->heads / d->kv_heads;
   const int64_t items = d->kv_heads * std::min<int64_t>((int64_t)d->sequences * ((d->max_k + bm - 1) / bm), d->total_k / bm + d->sequences);
-  const int64_t steps = (int64_t)(d->heads / d->kv_heads) * ((d->max_q + 31) / 32);
+  const int64_t steps = (int64_t)group * ((d->max_q + 31) / 32);
   const int64_t want = std::min((1024 + items - 1) / items, std::max((512 + items - 1) / items, steps / 96));
   const int64_t grid = (int64_t)d->sequences * ((d->max_k + bm - 1) / bm) * d->kv_heads;
-  return (int)std::max<int64_t>(1, std::min({want, steps / 8, kMaxGrid / grid}));
+  const int64_t chunks = std::max<int64_t>(1, std::min({want, steps / 8, kMaxGrid / grid}));
+  return (int)(d->num_buckets ? (chunks + group - 1) / group * group : chunks);  // with a bias none of two heads
 }
 size_t dist_bytes(const vc_packedattn_desc* d) {
   if (!d->num_buckets) return 0;
   const int bm = vcja::kPackedRows;
-  return align256((size_t)(vcja::dist_row(d->total_k, d->sequences, 0, bm) + 1) * d->heads * (2 * d->max_distance + 1) * sizeof(float));
+  const int per_head = key_chunks(d) / (d->heads / d->kv_heads);
+  return align256((size_t)(vcja::dist_row(d->total_k, d->sequences, 0, bm) + 1) * per_head * d->heads * (2 * d->max_distance + 1) *
+                  sizeof(float));
 }
 size_t key_part_bytes(const vc_packedattn_desc* d) {
   const int c = key_chunks(d);

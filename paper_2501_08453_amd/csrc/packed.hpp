@@ -39,7 +39,7 @@ struct PackedArgs {
   // packed_row(cu_q[s], s) on.
   float *nls, *dd;
   int npad;
-  float* dist_part;         // bias gradient: sums per distance, [dist_row][H][2 R + 1]
+  float* dist_part;         // bias gradient: sums per distance, [dist_row][Hkv][chunks][2 R + 1]
 };
 
 // A pointer that is the same for the whole wave, in scalar registers.

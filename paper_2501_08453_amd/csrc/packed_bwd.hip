@@ -292,7 +292,7 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedA
 
 // A key block's steps: query tiles [t0, t0 + nt) of every query head of its group, heads in
 // order; a call of several chunks gives each workgroup a run of them; with a bias
-// there are as many chunks as heads, each of one head.
+// the chunks are a multiple of the heads, each of one head.
 struct KeySteps {
   int t0, nt, u0, u1;
 };
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dkdv_kernel(Packe
     const int64_t r0 = dist_row(sr.k0, seq, b0 < sr.sk ? blk + 1 : 0, BM);
     const int64_t r1 = dist_row(min(max(__builtin_amdgcn_readfirstlane(a.cu_k[seq + 1]), 0), a.Tk), seq + 1, 0, BM);
     for (int64_t r = r0; r < r1; ++r)
-      for (int i = tid; i < 2 * a.R + 1; i += 64 * NW) a.dist_part[(r * a.H + kv * a.G + chunk) * (2 * a.R + 1) + i] = 0.0f;
+      for (int i = tid; i < 2 * a.R + 1; i += 64 * NW) a.dist_part[((r * a.Hkv + kv) * a.chunks + chunk) * (2 * a.R + 1) + i] = 0.0f;
   }
   if (b0 >= sr.sk) return;
   // Registers are the limit of the walk: what follows from the lane index is formed where it is
@@ -386,7 +386,7 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dkdv_kernel(Packe
                          (VC_LDS char*)smem + STAT + buf * 2 * SQ * 4 + (is_l ? 0 : SQ * 4));
   };
 
-  int g = BIAS ? chunk : __builtin_amdgcn_readfirstlane(ks.nt ? ks.u0 / ks.nt : 0), t = ks.u0 - g * ks.nt, buf = 0;  // scalar, as u0
+  int g = BIAS ? __builtin_amdgcn_readfirstlane(chunk / (a.chunks / a.G)) : __builtin_amdgcn_readfirstlane(ks.nt ? ks.u0 / ks.nt : 0), t = ks.u0 - g * ks.nt, buf = 0;  // scalar, as u0
   if (ks.u0 < ks.u1) {
     issue_stats(g, t, 0);
 #pragma unroll
@@ -582,7 +582,7 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dkdv_kernel(Packe
       hist[w * HIST + 2 * a.R] += up;
     }
     __syncthreads();
-    float* out = a.dist_part + (dist_row(sr.k0, seq, blk, BM) * a.H + kv * a.G + chunk) * (2 * a.R + 1);
+    float* out = a.dist_part + ((dist_row(sr.k0, seq, blk, BM) * a.Hkv + kv) * a.chunks + chunk) * (2 * a.R + 1);
     for (int i = tid; i < 2 * a.R + 1; i += 64 * NW) {
       float x = 0.0f;
 #pragma unroll
@@ -654,14 +654,15 @@ __global__ __launch_bounds__(1024) void packed_dbias_kernel(PackedArgs a, __bf16
   for (int d = tid; d < nd; d += 1024) bucket[d] = a.buckets[d];
   const int r0 = (int)dist_row(min(max(a.cu_k[0], 0), a.Tk), 0, 0, kPackedRows);
   const int r1 = (int)dist_row(min(max(a.cu_k[a.S], 0), a.Tk), a.S, 0, kPackedRows);
-  const float* rows = a.dist_part + (size_t)h * nd;
-  const size_t one = (size_t)a.H * nd;
+  const int k = a.chunks / a.G;  // chunks of one head: k rows of sums a block
+  const float* rows = a.dist_part + (size_t)h * k * nd;
+  const size_t one = (size_t)a.H * k * nd;
   for (int d0 = 0; d0 < nd; d0 += 1024) {
     const int n = min(nd - d0, 1024), runs = 1024 / n, run = tid / n, d = d0 + tid % n;
     float x = 0.0f;
     if (run < runs) {
 #pragma unroll 8
-      for (int r = r0 + run; r < r1; r += runs) x += rows[r * one + d];
+      for (int r = r0 * k + run; r < r1 * k; r += runs) x += rows[r / k * one + (size_t)(r % k) * nd + d];
     }
     part[tid] = x;
     __syncthreads();
