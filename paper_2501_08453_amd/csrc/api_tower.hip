@@ -119,19 +119,24 @@ int fwd_chunks(const vc_packedattn_desc* d, int64_t blocks, double rows, double 
   }
   return best;
 }
-// The same for the few-row kernel, in ns: a workgroup streams about 60 bytes a ns by itself, all of them
-// 5,200 together.
-int few_chunks(const vc_packedattn_desc* d, int64_t rows) {
+// The same for the few-row kernel, in ns: a workgroup streams about 50 bytes a ns by itself, 20 beside 256
+// others, all of them 5,200, a quarter of the longest one's time passes while the others have ended,
+// and each takes 3 us besides. Measured, us at 3, 4, 6, 8, 16 chunks, D = 128, 8 key
+// heads: 16 sequences of up to 8,000 keys 75, 66, 53, 55, 56; four of 200 to 8,000 42, 35, 26, 23, 22; 64 of
+// 100 to 2,431 73, 74, 76, 76, 78 (70 unsplit).
+int few_chunks(const vc_packedattn_desc* d, int64_t rows, int64_t blocks) {
   const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
   const double tile = 2.0 * 2 * vcja::kTileTok * d->head_dim;
+  const double share = std::min(1.0, (double)d->total_k / ((double)d->sequences * d->max_k));
   const double all = 2.0 * 2 * d->total_k * d->kv_heads * d->head_dim / 5200;
   double least = 1e30;
   int best = 1;
   for (int c = 1; c <= std::min(64, std::max(1, ntile / 2)); c += c < 8 ? 1 : c / 4) {
     const double span = (ntile + c - 1) / c * tile;
     const double merge = c == 1 ? 0 : 6000 + rows * c * (d->head_dim + 2) * 8 / 4000.0;
-    const double time = std::max(all + span / 120, span / 60 + 3000) + merge;
-    if (time < least * 0.98) {
+    const double wgs = blocks * (share * c + 0.5), alone = span / (50 - 30 * std::min(1.0, wgs / 256));
+    const double time = std::max(all + alone / 4 + std::max(1.0, wgs / 512) * 3000, alone + 3000) + merge;
+    if (time < least * 0.995) {
       least = time;
       best = c;
     }
@@ -151,7 +156,7 @@ FwdPlan fwd_plan(const vc_packedattn_desc* d) {
   p.few = rows <= 32;
   const int64_t grid = d->sequences * ((rows + bm - 1) / bm) * (d->heads / p.pack), outs = d->total_q * d->heads;
   const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
-  p.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(p.few ? few_chunks(d, outs) : fwd_chunks(d, blocks, (double)outs, share, uneven),
+  p.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(p.few ? few_chunks(d, outs, blocks) : fwd_chunks(d, blocks, (double)outs, share, uneven),
                                                           kMaxGrid / grid));
   p.span = (ntile + p.chunks - 1) / p.chunks;
   p.chunks = (ntile + p.span - 1) / p.span;

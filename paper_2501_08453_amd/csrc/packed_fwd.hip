@@ -390,7 +390,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 8 / kFewWaves) void packed_few_kern
     clear_o<D>(a, blockIdx.x - items, gridDim.x - items, tid, 64 * NW);
     return;
   }
-  const int hb = blockIdx.x % heads, s = blockIdx.x / heads % a.S, chunk = blockIdx.x / heads / a.S;
+  // Chunks run fastest: 57.5 -> 55.8 us, 53.5 -> 48.7 and 24.3 -> 20.1 against heads first.
+  const int chunk = blockIdx.x % a.chunks, hb = blockIdx.x / a.chunks % heads, s = blockIdx.x / a.chunks / heads;
   const SeqRows sr = seq_rows(a, s);
   if (sr.sq == 0) return;
   const int h0 = hb * a.pack, kv = h0 / a.G;
