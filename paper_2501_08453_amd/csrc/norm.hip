@@ -88,15 +88,21 @@ __global__ __launch_bounds__(kWg<TPR>) void norm_fwd_kernel(NormArgs a) {
   load_params<VE, NV, TPR>(a.w, a.p_f32, 1.0f, C, t, w);
   load_params<VE, NV, TPR>(a.b, a.p_f32, 0.0f, C, t, b);
   const int step = gridDim.x * (kWg<TPR> / TPR);
-  for (int row = blockIdx.x * (kWg<TPR> / TPR) + threadIdx.x / TPR; row < a.rows; row += step) {
+  R r[NV];
+  auto load = [&](int row, R* to) {
     const X* x = (const X*)a.x + row * a.stride;
-    R r[NV];
-    float s = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c = (v * TPR + t) * VE;
-      if (c < C) r[v] = *(const R*)(x + c);
+      if (c < C) to[v] = *(const R*)(x + c);
     }
+  };
+  int row = blockIdx.x * (kWg<TPR> / TPR) + threadIdx.x / TPR;
+  if (row < a.rows) load(row, r);
+  for (; row < a.rows; row += step) {
+    R next[NV];
+    if (row + step < a.rows) load(row + step, next);  // in flight during this row
+    float s = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v)
       if ((v * TPR + t) * VE < C)
@@ -134,6 +140,8 @@ __global__ __launch_bounds__(kWg<TPR>) void norm_fwd_kernel(NormArgs a) {
       a.mean[row] = mean;
       a.rstd[row] = rstd;
     }
+#pragma unroll
+    for (int v = 0; v < NV; ++v) r[v] = next[v];
   }
 }
 
@@ -370,8 +378,16 @@ void pick(int cols, bool vec, F go) {
     width(std::integral_constant<int, 1>{});
 }
 
-// Workgroups of a launch over rows (four to a workgroup up to kWaveCols columns).
-int row_groups(int64_t rows, int cols, int most) {
+// Workgroups of a launch over rows (four rows a workgroup up to kWaveCols columns), at most as many as
+// 256 compute units hold at once by the registers of the form (see pick), or fewer: a second round would
+// load the weights again and wait for its rows anew. Forward, 57,856 x 1,536 in bf16: 81.8 us at 1,024, 82.3 at
+// 2,048, 111 at 4,096; 20,000 x 4,096 69.5, 75.4, 93.8. Backward with the forward, 100,000 x 512: 113 us at 1,024,
+// 119 at 768, 137 at 512; 57,856 x 1,536 213, 229, 202; 20,000 x 4,096 218, 192, 195.
+int row_groups(int64_t rows, int cols, bool backward) {
+  const int most = cols > 6144                                  ? (backward ? 256 : 512)
+                   : cols <= 512 || (cols > 1536 && cols <= 2048) ? (backward ? 1024 : 2048)
+                   : cols <= 1024 || (cols > 1536 && cols <= 4096) ? (backward ? 768 : 1024)
+                                                                  : (backward ? 512 : 1024);
   return (int)std::min<int64_t>(most, cols <= kWaveCols ? (rows + 3) / 4 : rows);
 }
 
@@ -379,7 +395,7 @@ int row_groups(int64_t rows, int cols, int most) {
 
 int norm_groups(int64_t rows, int cols) {
   if (cols > kBlockCols) return (int)std::max<int64_t>(1, std::min<int64_t>(256, rows / 16));
-  return row_groups(rows, cols, 512);
+  return row_groups(rows, cols, true);
 }
 
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t s) {
@@ -395,7 +411,7 @@ hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t s) {
   const bool vec = a.cols % per == 0 && a.stride % per == 0 && aligned16(a.x) && aligned16(a.y);
   auto go = [&](auto x, auto ve, auto ept, auto tpr) {
     hipLaunchKernelGGL((norm_fwd_kernel<decltype(x), decltype(ve)::value, decltype(ept)::value, decltype(tpr)::value>),
-                       dim3(row_groups(a.rows, a.cols, 2048)), dim3(kWg<decltype(tpr)::value>), 0, s, a);
+                       dim3(row_groups(a.rows, a.cols, false)), dim3(kWg<decltype(tpr)::value>), 0, s, a);
   };
   if (a.x_f32)
     pick<float>(a.cols, vec, go);

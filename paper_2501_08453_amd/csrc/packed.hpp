@@ -103,18 +103,42 @@ __device__ __forceinline__ PackedItem packed_item(int x, int nblk, int Hkv, int 
 
 // Bias of one head per distance in LDS, divided by the softmax scale (the scores' own unit):
 // entry kBiasPad + R + d for distance d = key position - query position, distances past +-R
-// repeating the last, so that no tile that holds a distance inside (-R, R) reads outside.
+// repeating the last, so that no tile that holds a distance inside (-R, R) reads outside. The
+// kernels come with tables for distances up to 128 and up to kMaxBiasDistance, as the wide one
+// (and the sums per distance, backward) leaves room for fewer workgroups.
+constexpr int kSmallBiasDistance = 128;
 constexpr int kBiasPad = 96;  // >= 63 + 31, the distances in a tile of 64 keys x 32 queries
-constexpr int kBiasTable = 2 * kMaxBiasDistance + 1 + 2 * kBiasPad;
-__device__ __forceinline__ void load_bias_table(const PackedArgs& a, int h, float* tb, int tid, int threads) {
-  const float inv = 1.0f / a.scale;
-  for (int i = tid; i < 2 * a.R + 1 + 2 * kBiasPad; i += threads) {
-    const int u = a.buckets[min(max(i - kBiasPad, 0), 2 * a.R)];
-    float b = u >= 0 && u < a.nb ? (float)a.bias[(size_t)h * a.nb + u] : 0.0f;
-    b = b < -kBiasLimit ? -INFINITY : b > kBiasLimit ? kBiasLimit : b;  // a NaN stays one
-    tb[i] = b * inv;
+template <int RMAX>
+struct BiasTable {
+  static constexpr int N = 2 * RMAX + 1 + 2 * kBiasPad;
+  static constexpr int ROW = 256;  // buckets whose values are loaded along with the bucket numbers
+  float tb[N], row[ROW];
+  // By the whole workgroup; ends with the table readable.
+  __device__ __forceinline__ void load(const PackedArgs& a, int h, int tid, int threads) {
+    const __bf16* bias = a.bias + (size_t)h * a.nb;
+    const bool staged = a.nb <= ROW;
+    int u[(N + 255) / 256];
+#pragma unroll
+    for (int j = 0; j < (N + 255) / 256; ++j) u[j] = a.buckets[min(max(tid + j * threads - kBiasPad, 0), 2 * a.R)];
+    if (staged && tid < a.nb) row[tid] = (float)bias[tid];
+    __syncthreads();
+    const float inv = 1.0f / a.scale;
+#pragma unroll
+    for (int j = 0; j < (N + 255) / 256; ++j) {
+      const int i = tid + j * threads;
+      float b = 0.0f;
+      if (u[j] >= 0 && u[j] < a.nb) b = staged ? row[u[j]] : (float)bias[u[j]];
+      b = b < -kBiasLimit ? -INFINITY : b > kBiasLimit ? kBiasLimit : b;  // a NaN stays one
+      if (i < N) tb[i] = b * inv;
+    }
+    __syncthreads();
   }
-}
+};
+template <>
+struct BiasTable<0> {  // no bias
+  float tb[1];
+  __device__ __forceinline__ void load(const PackedArgs&, int, int, int) {}
+};
 
 // Where a block of keys [k0, k1] stands to a block of query positions [p0, p1]: every distance
 // at or past R (1), at or before -R (-1), or some inside (0).

@@ -9,7 +9,7 @@
 //   K and V of its keys in registers, and walks over the query tiles of 32 of every query head
 //   of the group, so that dK and dV of the shared head are summed in registers; where that leaves
 //   too few workgroups, each takes a run of those tiles and fp32 partials are summed afterwards.
-//   With a bias it also sums dS over every distance (see distance_sums).
+//   With a bias it also sums dS over every distance, in LDS.
 // No atomics anywhere: results are bitwise reproducible.
 #include "packed.hpp"
 
@@ -26,24 +26,27 @@ __device__ __forceinline__ bf16x8 operand(const f32x16& x, int half) {
   return y;
 }
 
-// Sums of one 32 queries x 32 keys block of dS over its diagonals (distance = key - query), without
-// atomics. Register r of a lane of half hi holds query row n = 8 (r / 4) + 4 hi + r % 4 of its
-// key: rotating it by n brings distance t (where n + t < 32) or t - 32 to lane t, the same for
-// every register, so that a lane adds its own values up; the two halves of the wave are joined
-// at the end, the lower one keeping distances 0 .. 31, the upper one -32 .. -1.
+// Sums of one 32 queries x 32 keys block of dS over its diagonals (distance = key - query). Register r of
+// a lane of half hi holds query row n = 8 (r / 4) + 4 hi + r % 4 of its key: rotating it by n brings
+// distance t (where n + t < 32) or t - 32 to lane t, the same for every register, so that a lane adds
+// its own values up; the two halves of the wave are joined at the end, the lower one keeping
+// distances 0 .. 31, the upper one -32 .. -1 (as the sum of all less those: exact to the fp32 sums'
+// own rounding). Additions in LDS (ds_add_f32) took three times as long as the whole walk: 32 -> 104 us
+// at captions of 8 to 256 tokens.
 __device__ __forceinline__ float distance_sums(const f32x16& ds, int lane) {
-  const int t = lane & 31, hi = lane >> 5;
-  float pos = 0.0f, neg = 0.0f;
+  const int t = lane & 31, hi = lane >> 5, y = t + 4 * hi;
+  float pos = 0.0f, all = 0.0f;
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
     if (r % 4 == 0) sched_fence();  // a few at a time: registers are the limit here
-    const int n = acc_row(r, hi);
-    const float x = __shfl(ds[r], (lane & 32) | ((n + t) & 31), 64);
-    pos += n + t < 32 ? x : 0.0f;
-    neg += n + t < 32 ? 0.0f : x;
+    const int n = 8 * (r >> 2) + (r & 3);
+    const int from = ((4 * y + 4 * n) & 124) | (4 * (lane & 32));
+    const float x = __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(from, __builtin_bit_cast(int, (float)ds[r])));
+    all += x;
+    pos += y < 32 - n ? x : 0.0f;
   }
+  const float neg = halves_sum(all - pos);
   pos = halves_sum(pos);
-  neg = halves_sum(neg);
   return hi ? neg : pos;
 }
 
@@ -67,7 +70,7 @@ __device__ __forceinline__ void clear_rows(__bf16* x, __bf16* y, const int32_t* 
   }
 }
 
-template <int D, bool BIAS>
+template <int D, int RMAX>
 __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedArgs a) {
   using Rows = SwzRows<D>;
   using Reads = SwzReads<D>;
@@ -76,7 +79,9 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedA
   constexpr int STAGE = 2 * RT;                  // K | V rows of a tile
   constexpr int CPW = kBN / Rows::RPC / NW;      // copies of each per wave
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
-  __shared__ float tb[BIAS ? kBiasTable : 1];
+  __shared__ BiasTable<RMAX> table;
+  constexpr bool BIAS = RMAX > 0;
+  const float* const tb = table.tb;
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -140,7 +145,7 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedA
     const float x = a.lse[(size_t)it.h * a.Tq + row];
     nls = klim == 0 || x == -INFINITY ? -INFINITY : -x / a.scale;
   }
-  if (BIAS) load_bias_table(a, it.h, tb, tid, 64 * NW);
+  table.load(a, it.h, tid, 64 * NW);
 
   f32x16 acc[D / 32];
 #pragma unroll
@@ -307,7 +312,7 @@ __device__ __forceinline__ KeySteps key_steps(const PackedArgs& a, const SeqRows
   return k;
 }
 
-template <int D, bool BIAS>
+template <int D, int RMAX>
 __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dkdv_kernel(PackedArgs a) {
   using Rows = SwzRows<D>;
   using Reads = SwzReads<D>;
@@ -318,11 +323,13 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dkdv_kernel(Packe
   constexpr int CPW = 2 * COPIES / NW;        // copies per wave and tile, Q's first
   constexpr int STAT = 2 * STAGE;             // -LSE/c | -D of a run of SQ queries, two buffers
   constexpr int SQ = 256, SPT = SQ / kBQ;
-  constexpr int HIST = 2 * kMaxBiasDistance + 1;
+  // Sums of dS per distance: each wave's inside (-R, R), each lane's up to -R and from R on.
+  constexpr int HIST = 2 * RMAX + 1;
   __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE + 2 * 2 * SQ * 4];
-  __shared__ float tb[BIAS ? kBiasTable : 1];
-  __shared__ float hist[BIAS ? NW * HIST : 1];  // each wave's sums of dS per distance inside (-R, R),
-  __shared__ float ends[BIAS ? NW * 128 : 1];   // each lane's of those up to -R and from R on
+  __shared__ BiasTable<RMAX> table;
+  constexpr bool BIAS = RMAX > 0;
+  const float* const tb = table.tb;
+  __shared__ float hist[RMAX ? NW * HIST : 1], ends[RMAX ? NW * 128 : 1];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -403,10 +410,9 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dkdv_kernel(Packe
     }
   }
   if (BIAS) {
-    load_bias_table(a, kv * a.G + g, tb, tid, 64 * NW);
     for (int i = tid; i < NW * HIST; i += 64 * NW) hist[i] = 0.0f;
     for (int i = tid; i < NW * 128; i += 64 * NW) ends[i] = 0.0f;
-    __syncthreads();  // also where no step follows
+    table.load(a, kv * a.G + g, tid, 64 * NW);  // its barriers cover the sums too, also where no step follows
   }
   wait_all_memory();  // the loads above too: no later wait stands among copies
 
@@ -575,15 +581,23 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dkdv_kernel(Packe
   }
   wait_all_memory();  // no copy outlives the workgroup
   if (BIAS) {  // the head's sums per distance, waves in order
-    const int ln = fresh_lane();
-    const float lo = wave_sum(ends[w * 128 + ln]), up = wave_sum(ends[w * 128 + 64 + ln]);
-    if (ln == 0) {
-      hist[w * HIST] += lo;
-      hist[w * HIST + 2 * a.R] += up;
-    }
     __syncthreads();
-    float* out = a.dist_part + ((dist_row(sr.k0, seq, blk, BM) * a.Hkv + kv) * a.chunks + chunk) * (2 * a.R + 1);
-    for (int i = tid; i < 2 * a.R + 1; i += 64 * NW) {
+    const int ln = fresh_lane(), nd = 2 * a.R + 1;
+    float* out = a.dist_part + ((dist_row(sr.k0, seq, blk, BM) * a.Hkv + kv) * a.chunks + chunk) * nd;
+    auto end_sum = [&](int side) {
+      float x = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NW; ++j) x += ends[j * 128 + side * 64 + ln];
+      return wave_sum(x);
+    };
+    if (w == 0) {  // with R = 0 one distance stands for all
+      const float x = a.R == 0 ? end_sum(0) + end_sum(1) : end_sum(0);
+      if (ln == 0) out[0] = x;
+    } else if (w == 1 && a.R > 0) {
+      const float x = end_sum(1);
+      if (ln == 0) out[nd - 1] = x;
+    }
+    for (int i = 1 + tid; i < nd - 1; i += 64 * NW) {
       float x = 0.0f;
 #pragma unroll
       for (int j = 0; j < NW; ++j) x += hist[j * HIST + i];
@@ -661,8 +675,9 @@ __global__ __launch_bounds__(1024) void packed_dbias_kernel(PackedArgs a, __bf16
     const int n = min(nd - d0, 1024), runs = 1024 / n, run = tid / n, d = d0 + tid % n;
     float x = 0.0f;
     if (run < runs) {
+      for (int j = 0; j < k; ++j)
 #pragma unroll 8
-      for (int r = r0 * k + run; r < r1 * k; r += runs) x += rows[r / k * one + (size_t)(r % k) * nd + d];
+        for (int r = r0 + run; r < r1; r += runs) x += rows[r * one + (size_t)j * nd + d];
     }
     part[tid] = x;
     __syncthreads();
@@ -694,31 +709,36 @@ __global__ __launch_bounds__(1024) void packed_dbias_kernel(PackedArgs a, __bf16
 }  // namespace
 
 namespace {
-template <int D, bool BIAS>
+template <int D, int RMAX>
 void launch_bwd(PackedArgs a, __bf16* dbias, int clear, hipStream_t s) {
   const dim3 block(64 * kPackedWaves);
   a.nblk = (a.max_q + kPackedRows - 1) / kPackedRows;
-  hipLaunchKernelGGL((packed_dq_kernel<D, BIAS>), dim3(a.nblk * a.H * a.S + clear), block, 0, s, a);
+  hipLaunchKernelGGL((packed_dq_kernel<D, RMAX>), dim3(a.nblk * a.H * a.S + clear), block, 0, s, a);
   a.nblk = (a.max_k + kPackedRows - 1) / kPackedRows;
-  hipLaunchKernelGGL((packed_dkdv_kernel<D, BIAS>), dim3(a.nblk * a.Hkv * a.S * a.chunks + clear), block, 0, s, a);
+  hipLaunchKernelGGL((packed_dkdv_kernel<D, RMAX>), dim3(a.nblk * a.Hkv * a.S * a.chunks + clear), block, 0, s, a);
   if (a.chunks > 1) {
     const size_t threads = (size_t)a.Tk * a.Hkv * D / 4;
     hipLaunchKernelGGL(packed_key_sum_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, a.Hkv * D);
   }
-  if (BIAS && dbias) hipLaunchKernelGGL(packed_dbias_kernel, dim3(a.H), dim3(1024), 0, s, a, dbias);
+  if (RMAX && dbias) hipLaunchKernelGGL(packed_dbias_kernel, dim3(a.H), dim3(1024), 0, s, a, dbias);
 }
 }  // namespace
 
 hipError_t launch_packed_bwd(const PackedArgs& a, int head_dim, __bf16* dbias, hipStream_t s) {
   const int clear = a.clear ? 32 : 0;
-  if (head_dim == 128 && a.bias)
-    launch_bwd<128, true>(a, dbias, clear, s);
+  const int rmax = !a.bias ? 0 : a.R <= kSmallBiasDistance ? kSmallBiasDistance : kMaxBiasDistance;
+  if (head_dim == 128 && rmax == 0)
+    launch_bwd<128, 0>(a, dbias, clear, s);
+  else if (head_dim == 128 && rmax == kSmallBiasDistance)
+    launch_bwd<128, kSmallBiasDistance>(a, dbias, clear, s);
   else if (head_dim == 128)
-    launch_bwd<128, false>(a, dbias, clear, s);
-  else if (a.bias)
-    launch_bwd<64, true>(a, dbias, clear, s);
+    launch_bwd<128, kMaxBiasDistance>(a, dbias, clear, s);
+  else if (rmax == 0)
+    launch_bwd<64, 0>(a, dbias, clear, s);
+  else if (rmax == kSmallBiasDistance)
+    launch_bwd<64, kSmallBiasDistance>(a, dbias, clear, s);
   else
-    launch_bwd<64, false>(a, dbias, clear, s);
+    launch_bwd<64, kMaxBiasDistance>(a, dbias, clear, s);
   return hipGetLastError();
 }
 

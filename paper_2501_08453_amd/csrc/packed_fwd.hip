@@ -99,7 +99,7 @@ __device__ __forceinline__ void write_partial(const PackedArgs& a, int chunk, in
 
 // The query rows of a workgroup: row r is query r / pack, head r % pack of its block of heads
 // (pack = 1: one head; pack = the group: its heads share every tile of keys).
-template <int D, bool BIAS>
+template <int D, int RMAX>
 __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_fwd_kernel(PackedArgs a) {
   using Rows = SwzRows<D>;
   using Reads = SwzReads<D>;
@@ -107,7 +107,9 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_fwd_kernel(Packed
   constexpr int KT = Rows::bytes(kBN);
   constexpr int CPW = kBN / Rows::RPC / NW;  // copies of a K (V) tile per wave
   __shared__ __attribute__((aligned(1024))) char smem[4 * KT];  // K ring | V ring
-  __shared__ float tb[BIAS ? kBiasTable : 1];
+  __shared__ BiasTable<RMAX> table;
+  constexpr bool BIAS = RMAX > 0;
+  const float* const tb = table.tb;
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -169,7 +171,7 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_fwd_kernel(Packed
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const bf16x8*)(qp + 16 * ks);
   }
-  if (BIAS) load_bias_table(a, h0, tb, tid, 64 * NW);
+  table.load(a, h0, tid, 64 * NW);
 
   const int krow = Reads::row_base(l32, hi), vtr = Reads::tr_base(lane);
   const int pos0 = w0 + sr.off;  // position of the wave's first query (with a bias: pack = 1)
@@ -367,7 +369,7 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_fwd_kernel(Packed
 // LDS of its own without a barrier, the next tile's keys in flight once the scores are formed, its
 // values once they are used, eight waves a compute unit; their results are joined in LDS at the
 // end.
-template <int D, bool BIAS>
+template <int D, int RMAX>
 __global__ __launch_bounds__(64 * kFewWaves, 8 / kFewWaves) void packed_few_kernel(PackedArgs a) {
   using Rows = SwzRows<D>;
   using Reads = SwzReads<D>;
@@ -379,7 +381,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 8 / kFewWaves) void packed_few_kern
   static_assert(RING >= 32 * OS * 4, "O of a wave fits its ring");
   __shared__ __attribute__((aligned(1024))) char smem[NW * RING];
   __shared__ float ml[NW][32][2];
-  __shared__ float tb[BIAS ? kBiasTable : 1];
+  __shared__ BiasTable<RMAX> table;
+  constexpr bool BIAS = RMAX > 0;
+  const float* const tb = table.tb;
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -434,10 +438,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 8 / kFewWaves) void packed_few_kern
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) qf[ks] = *(const bf16x8*)(qp + 16 * ks);
   }
-  if (BIAS) {
-    load_bias_table(a, h0, tb, tid, 64 * NW);
-    __syncthreads();
-  }
+  table.load(a, h0, tid, 64 * NW);
   wait_all_memory();
 
   f32x16 oacc[D / 32];
@@ -614,14 +615,14 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedArgs a) {
   if (lane == 0) a.lse[(size_t)h * a.Tq + sr.q0 + i] = sum == 0.0f ? -INFINITY : (mx + log2f(sum)) * kLn2;
 }
 
-template <int D, bool BIAS>
+template <int D, int RMAX>
 void launch(PackedArgs a, hipStream_t s) {
   const int clear = a.clear ? 32 : 0, heads = a.H / a.pack;
   if (a.few) {
-    hipLaunchKernelGGL((packed_few_kernel<D, BIAS>), dim3(heads * a.S * a.chunks + clear), dim3(64 * kFewWaves), 0, s, a);
+    hipLaunchKernelGGL((packed_few_kernel<D, RMAX>), dim3(heads * a.S * a.chunks + clear), dim3(64 * kFewWaves), 0, s, a);
   } else {
     a.nblk = (a.max_q * a.pack + kPackedRows - 1) / kPackedRows;
-    hipLaunchKernelGGL((packed_fwd_kernel<D, BIAS>), dim3(a.nblk * heads * a.S * a.chunks + clear), dim3(64 * kPackedWaves), 0, s, a);
+    hipLaunchKernelGGL((packed_fwd_kernel<D, RMAX>), dim3(a.nblk * heads * a.S * a.chunks + clear), dim3(64 * kPackedWaves), 0, s, a);
   }
   if (a.chunks > 1) hipLaunchKernelGGL(packed_merge_kernel<D>, dim3((a.S * a.max_q * a.H + 3) / 4), dim3(256), 0, s, a);
 }
@@ -629,14 +630,19 @@ void launch(PackedArgs a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_packed_fwd(const PackedArgs& a, int head_dim, hipStream_t s) {
-  if (head_dim == 128 && a.bias)
-    launch<128, true>(a, s);
+  const int rmax = !a.bias ? 0 : a.R <= kSmallBiasDistance ? kSmallBiasDistance : kMaxBiasDistance;
+  if (head_dim == 128 && rmax == 0)
+    launch<128, 0>(a, s);
+  else if (head_dim == 128 && rmax == kSmallBiasDistance)
+    launch<128, kSmallBiasDistance>(a, s);
   else if (head_dim == 128)
-    launch<128, false>(a, s);
-  else if (a.bias)
-    launch<64, true>(a, s);
+    launch<128, kMaxBiasDistance>(a, s);
+  else if (rmax == 0)
+    launch<64, 0>(a, s);
+  else if (rmax == kSmallBiasDistance)
+    launch<64, kSmallBiasDistance>(a, s);
   else
-    launch<64, false>(a, s);
+    launch<64, kMaxBiasDistance>(a, s);
   return hipGetLastError();
 }
 
