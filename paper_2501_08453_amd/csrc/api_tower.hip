@@ -99,10 +99,11 @@ struct FwdPlan {
 // of that at 64, with two workgroups a compute unit): rounds over 512 places, each workgroup 3 tiles
 // more than its keys for its start and its partial results, and the merge, a launch of about 6 us and
 // the partials' way to memory and back. `share`: mean over longest keys of a block; `uneven` blocks (the
-// causal rule's, longest first) fill their last round. Measured, us at 1, 2, 4, 8, 16 chunks (32 heads, 8 key heads, D = 128): 512 queries behind 16,384
+// causal rule's, longest first) fill their last round. `cost`:
+// receives the estimated time unsplit over the least. Measured, us at 1, 2, 4, 8, 16 chunks (32 heads, 8 key heads, D = 128): 512 queries behind 16,384
 // keys -, -, 144, 157, 181; 128 behind 16,384 -, -, -, -, 57 (74 at 32); 4 x 64 behind 500 to 9,000 -, -, 62, 46,
 // 57; 8,192 causal at 4 heads 134, 113, 110, 107; two texts of 12 heads at D = 64 41, 48, 45 (3), 51 (5).
-int fwd_chunks(const vc_packedattn_desc* d, int64_t blocks, double rows, double share, bool uneven) {
+int fwd_chunks(const vc_packedattn_desc* d, int64_t blocks, double rows, double share, bool uneven, double* cost = nullptr) {
   const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
   const double tile_us = d->head_dim == 128 ? 1.8 : 0.9;
   double least = 1e30;
@@ -116,7 +117,9 @@ int fwd_chunks(const vc_packedattn_desc* d, int64_t blocks, double rows, double 
       least = time;
       best = c;
     }
+    if (cost && c == 1) *cost = time;
   }
+  if (cost) *cost /= least;
   return best;
 }
 // The same for the few-row kernel, in ns: a workgroup streams about 50 bytes a ns by itself, 20 beside 256
@@ -167,6 +170,32 @@ size_t fwd_part_bytes(const vc_packedattn_desc* d) {
   return p.chunks == 1 ? 256 : align256((size_t)p.chunks * d->total_q * d->heads * (d->head_dim + 2) * sizeof(float));
 }
 
+// The dQ pass's chunks of a row block's key tiles: as the forward's, where they promise to take less than
+// 0.7 of the time. Forward and backward, us unsplit / split, 16 heads, D = 128: 64 queries of 16,384 keys 350 / 93, 300
+// and 200 of 8,000 and 3,000 324 / 253, 8,192 causal at 4 heads 435 / 420; not so 2,048 causal 159 / 168, 4,096 389 / 410.
+struct DqPlan {
+  int chunks, span;
+};
+DqPlan dq_plan(const vc_packedattn_desc* d) {
+  const int64_t bm = vcja::kPackedRows, per = (d->max_q + bm - 1) / bm;
+  const int64_t blocks = std::min<int64_t>(d->sequences * per, d->total_q / bm + d->sequences) * d->heads;
+  double share = std::min(1.0, (double)d->total_k / ((double)d->sequences * d->max_k));
+  const bool uneven = d->causal && 2 * (int64_t)d->max_q > d->max_k;
+  if (uneven) share *= 0.5;
+  const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
+  double gain = 1;
+  int64_t chunks = fwd_chunks(d, blocks, (double)d->total_q * d->heads, share, uneven, &gain);
+  chunks = gain * 0.7 < 1 ? 1 : std::max<int64_t>(1, std::min(chunks, kMaxGrid / (d->sequences * per * d->heads)));
+  DqPlan p;
+  p.span = (int)((ntile + chunks - 1) / chunks);
+  p.chunks = (ntile + p.span - 1) / p.span;
+  return p;
+}
+size_t dq_part_bytes(const vc_packedattn_desc* d) {
+  const int c = dq_plan(d).chunks;
+  return c == 1 ? 0 : align256((size_t)c * d->total_q * d->heads * (d->head_dim + 1) * sizeof(float));
+}
+
 // Backward workspace: -LSE/c | -D | the bias gradient's sums per distance.
 size_t stat_bytes(const vc_packedattn_desc* d) {
   return align256((size_t)d->heads * vcja::packed_rows(d->total_q, d->sequences) * sizeof(float));
@@ -195,6 +224,11 @@ size_t dist_bytes(const vc_packedattn_desc* d) {
 size_t key_part_bytes(const vc_packedattn_desc* d) {
   const int c = key_chunks(d);
   return c == 1 ? 0 : align256((size_t)c * 2 * d->total_k * d->kv_heads * d->head_dim * sizeof(float));
+}
+
+// The partial results of the two passes take the same room, one after the other.
+size_t bwd_ws_bytes(const vc_packedattn_desc* d) {
+  return 2 * stat_bytes(d) + dist_bytes(d) + std::max(key_part_bytes(d), dq_part_bytes(d));
 }
 
 vc_status check_inputs(const vc_packedattn_desc* d, const void* q, const void* k, const void* v, const int32_t* cu_q,
@@ -245,7 +279,7 @@ vc_status vc_packedattn_fwd(const vc_packedattn_desc* desc, const void* q, const
 }
 
 size_t vc_packedattn_bwd_workspace_bytes(const vc_packedattn_desc* desc) {
-  return check_packed(desc) == VC_OK ? 2 * stat_bytes(desc) + dist_bytes(desc) + key_part_bytes(desc) : 0;
+  return check_packed(desc) == VC_OK ? bwd_ws_bytes(desc) : 0;
 }
 
 vc_status vc_packedattn_bwd(const vc_packedattn_desc* desc, const void* q, const void* k, const void* v, const void* o,
@@ -274,7 +308,11 @@ vc_status vc_packedattn_bwd(const vc_packedattn_desc* desc, const void* q, const
   a.dd = reinterpret_cast<float*>(ws + stat_bytes(desc));
   a.dist_part = reinterpret_cast<float*>(ws + 2 * stat_bytes(desc));
   a.key_part = reinterpret_cast<float*>(ws + 2 * stat_bytes(desc) + dist_bytes(desc));
+  a.part = a.key_part;
   a.chunks = key_chunks(desc);
+  const DqPlan p = dq_plan(desc);
+  a.dq_chunks = p.chunks;
+  a.span = p.span;
   return vcja::launch_packed_bwd(a, desc->head_dim, static_cast<__bf16*>(dbias), as_stream(stream)) == hipSuccess ? VC_OK
                                                                                                             : VC_ERR_HIP;
 }

@@ -31,9 +31,11 @@ struct PackedArgs {
   float scale, scale_log2;  // softmax scale; times log2(e)
   int nblk;                 // row blocks of the longest slot
   int chunks;               // workgroups that share a row block's key tiles (backward: a key block's query tiles)
-  int pack, span;           // forward: heads of a group in one row block; key tiles of a chunk
+  int dq_chunks;            // backward: workgroups that share a row block's key tiles
+  int pack, span;           // forward: heads of a group in one row block; key tiles of a chunk (dQ pass: of dq_chunks)
   bool few;                 // forward: all rows of a (sequence, key head) in one wave's 32
-  float* part;              // forward: the chunks' partial results (see write_partial)
+  float* part;              // forward: the chunks' partial results (see write_partial); dQ pass: [dq_chunks][Tq, H][D] of
+                            // dQ / scale, then [dq_chunks][Tq, H] sums of dS
   float* key_part;          // their partial dK, dV: [chunks][2][Tk, Hkv, D]
   // Backward: per query row -LSE / c (-inf on padding) and -D, [H, npad], sequence s from row
   // packed_row(cu_q[s], s) on.

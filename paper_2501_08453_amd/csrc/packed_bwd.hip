@@ -4,7 +4,7 @@
 //   (sequence, head), each wave 32, with Q^T and dO^T of its queries in registers. It forms
 //   D_i = <dO_i, O_i> from its own rows and walks over the key tiles like the forward, computing
 //   S^T, dP^T and dS^T = P^T o (dP^T - D), and dQ^T += K^T dS^T. It leaves -LSE / c and -D for the
-//   other pass.
+//   other pass. Few queries before many keys: several workgroups share a block's key tiles.
 // dK/dV (key-stationary): one workgroup owns 128 keys of one (sequence, key head), each wave 32,
 //   K and V of its keys in registers, and walks over the query tiles of 32 of every query head
 //   of the group, so that dK and dV of the shared head are summed in registers; where that leaves
@@ -87,12 +87,13 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedA
   const int lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hi = lane >> 5;
-  const int items = a.nblk * a.H * a.S;
+  const int blocks = a.nblk * a.H * a.S, items = blocks * a.dq_chunks;
   if ((int)blockIdx.x >= items) {
     clear_rows<D>(a.dq, nullptr, a.cu_q, a.S, a.Tq, a.H, blockIdx.x - items, gridDim.x - items, tid, 64 * NW);
     return;
   }
-  const PackedItem it = packed_item(blockIdx.x, a.nblk, a.Hkv, a.G, a.S);
+  const int chunk = (int)blockIdx.x / blocks;  // of the block's key tiles
+  const PackedItem it = packed_item(blockIdx.x % blocks, a.nblk, a.Hkv, a.G, a.S);
   const SeqRows sr = seq_rows(a, it.s);
   const int b0 = it.blk * BM;
   if (b0 >= sr.sq) return;
@@ -104,7 +105,8 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedA
   const int wave_keys = b0 + w * 32 < qe ? limit(min(b0 + w * 32 + 32, sr.nq) - 1) : 0;
   const int wave_all = limit(b0 + w * 32);
   const int klim = qi < sr.nq ? limit(qi) : 0;
-  const int ntile = (blk_keys + kBN - 1) / kBN;
+  const int ntile = (blk_keys + kBN - 1) / kBN, kt0 = chunk * a.span, kt1 = min(ntile, kt0 + a.span);
+  if (chunk > 0 && kt0 >= kt1) return;
 
   const SwzCopy<D, true> kc(a.k_tok, lane), vc(a.v_tok, lane);
   const __bf16* kbase = a.k + (size_t)sr.k0 * a.k_tok + kv * D;
@@ -125,7 +127,7 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedA
     }
   };
 
-  if (ntile > 0) issue_tile(0, 0);  // in flight with the loads below
+  if (kt0 < kt1) issue_tile(kt0, 0);  // in flight with the loads below
   bf16x8 qf[D / 16], dof[D / 16];
   float nls, dd;
   {
@@ -155,12 +157,12 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedA
   float rowsum = 0.0f;
 
   wait_all_memory();  // the loads above too: no later wait stands among copies
-  for (int kt = 0; kt < ntile; ++kt) {
-    const int st = kt & 1;
+  for (int kt = kt0; kt < kt1; ++kt) {
+    const int st = (kt - kt0) & 1;
     wait_all_memory();
     __syncthreads();
     const int k0 = kt * kBN;
-    const int kn = min(kt + 1, ntile - 1);  // past the last tile: copied again, never read
+    const int kn = min(kt + 1, kt1 - 1);  // past the last tile: copied again, never read
     if (k0 >= wave_keys) {
       issue_tile(kn, st ^ 1);
       continue;
@@ -275,11 +277,23 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedA
 
   // What dS of a row sums up to beside 0 is the error of its D, taken of the rounded O: the other
   // pass gets D without it. (Rows past the sequence's own: inert.)
+  const bool split = ntile > a.span;  // several workgroups: the sum kernel finishes dQ and D
   rowsum = halves_sum(rowsum);
-  if (hi == 0 && qi < ((sr.nq + 63) & ~63)) {
+  if (chunk == 0 && hi == 0 && qi < ((sr.nq + 63) & ~63)) {
     const size_t p = (size_t)it.h * a.npad + packed_row(sr.q0, it.s) + qi;
     a.nls[p] = nls;
-    a.dd[p] = klim == 0 ? 0.0f : dd - rowsum;
+    a.dd[p] = klim == 0 ? 0.0f : split ? dd : dd - rowsum;
+  }
+  if (split && qi < sr.sq) {
+    const size_t rows = (size_t)a.Tq * a.H, at = chunk * rows + (size_t)(sr.q0 + qi) * a.H + it.h;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *(f32x4*)(a.part + at * D + db * 32 + 8 * j + 4 * hi) =
+            f32x4{acc[db][4 * j + 0], acc[db][4 * j + 1], acc[db][4 * j + 2], acc[db][4 * j + 3]};
+    if (hi == 0) a.part[a.dq_chunks * rows * D + at] = rowsum;
+    return;
   }
   if (qi < sr.sq) {  // rows that see no key, and rows of the slot past the sequence's own: 0
     __bf16* qp = a.dq + ((size_t)(sr.q0 + qi) * a.H + it.h) * D;
@@ -293,6 +307,40 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedA
         *(bf16x4*)(qp + db * 32 + 8 * j + 4 * hi) = t;
       }
   }
+}
+
+// dQ, and -D without the sums of dS, of the rows whose keys several workgroups share, in order. One wave per
+// (query, head).
+template <int D>
+__global__ __launch_bounds__(256) void packed_dq_sum_kernel(PackedArgs a) {
+  constexpr int E = D / 64;
+  typedef float fe __attribute__((ext_vector_type(E)));
+  const int lane = threadIdx.x & 63;
+  const int x = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  if (x >= a.S * a.max_q * a.H) return;
+  const int h = x % a.H, i = x / a.H % a.max_q, s = x / a.H / a.max_q;
+  const SeqRows sr = seq_rows(a, s);
+  if (i >= sr.sq) return;
+  // The tiles of the row's block of rows, as the dQ kernel counts them.
+  auto limit = [&](int q) { return a.causal ? max(0, min(sr.nk, q + sr.off + 1)) : sr.nk; };
+  const int b0 = i / kPackedRows * kPackedRows, qe = min(b0 + kPackedRows, sr.nq);
+  const int n = ((qe > b0 ? limit(qe - 1) : 0) + kBN - 1) / kBN;
+  if (n <= a.span) return;  // written by its only workgroup
+  const int chunks = (n + a.span - 1) / a.span;
+  const size_t rows = (size_t)a.Tq * a.H, at = (size_t)(sr.q0 + i) * a.H + h;
+  const bool sees = i < sr.nq && limit(i) > 0;
+  fe acc;
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+  float sum = 0.0f;
+#pragma unroll 4
+  for (int c = 0; c < chunks; ++c) {
+    acc += *(const fe*)(a.part + (c * rows + at) * D + E * lane);
+    sum += a.part[a.dq_chunks * rows * D + c * rows + at];
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) a.dq[at * D + E * lane + e] = (__bf16)(sees ? acc[e] * a.scale : 0.0f);
+  if (lane == 0 && sees) a.dd[(size_t)h * a.npad + packed_row(sr.q0, s) + i] -= sum;
 }
 
 // A key block's steps: query tiles [t0, t0 + nt) of every query head of its group, heads in
@@ -713,7 +761,8 @@ template <int D, int RMAX>
 void launch_bwd(PackedArgs a, __bf16* dbias, int clear, hipStream_t s) {
   const dim3 block(64 * kPackedWaves);
   a.nblk = (a.max_q + kPackedRows - 1) / kPackedRows;
-  hipLaunchKernelGGL((packed_dq_kernel<D, RMAX>), dim3(a.nblk * a.H * a.S + clear), block, 0, s, a);
+  hipLaunchKernelGGL((packed_dq_kernel<D, RMAX>), dim3(a.nblk * a.H * a.S * a.dq_chunks + clear), block, 0, s, a);
+  if (a.dq_chunks > 1) hipLaunchKernelGGL(packed_dq_sum_kernel<D>, dim3((a.S * a.max_q * a.H + 3) / 4), dim3(256), 0, s, a);
   a.nblk = (a.max_k + kPackedRows - 1) / kPackedRows;
   hipLaunchKernelGGL((packed_dkdv_kernel<D, RMAX>), dim3(a.nblk * a.Hkv * a.S * a.chunks + clear), block, 0, s, a);
   if (a.chunks > 1) {
