@@ -17,7 +17,7 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 inline const __bf16* bf(const void* p) { return static_cast<const __bf16*>(p); }
 
-constexpr int64_t kMaxGrid = (int64_t)1 << 30;    // workgroups of one launch
+constexpr int64_t kMaxGrid = (int64_t)1 << 30;    // workgroups of one launch, waves of a merge
 constexpr int64_t kMaxRows = (int64_t)1 << 30;
 constexpr int64_t kMaxStride = (int64_t)1 << 23;  // elements between tokens: tile offsets of 16 rows stay in 32 bits
 
@@ -90,6 +90,18 @@ vcja::PackedArgs packed_args(const vc_packedattn_desc* d, const void* q, const v
   return a;
 }
 
+// Blocks of kPackedRows rows (slots of up to `longest`, `total` in all) as so many of the longest slot's, if the
+// other S - 1 sequences share the rest evenly and a block takes time by the other side's tokens.
+double equal_blocks(const vc_packedattn_desc* d, int64_t longest, int64_t total, int64_t other_longest, int64_t other_total) {
+  const double bm = vcja::kPackedRows, rest = d->sequences - 1;
+  double blocks = ceil(longest / bm);
+  if (rest > 0) {
+    const double mean = std::max<int64_t>(0, total - longest) / rest, other = std::max<int64_t>(0, other_total - other_longest) / rest;
+    blocks += rest * ceil(mean / bm) * std::min(1.0, other / other_longest);
+  }
+  return blocks;
+}
+
 // Forward: heads of a group packed into a row block, and the chunks of a row block's key tiles.
 struct FwdPlan {
   int pack, chunks, span;
@@ -98,19 +110,19 @@ struct FwdPlan {
 // The chunks of least estimated time, in tiles of 64 keys x 128 rows (about 1.8 us at head_dim 128, half
 // of that at 64, with two workgroups a compute unit): rounds over 512 places, each workgroup 3 tiles
 // more than its keys for its start and its partial results, and the merge, a launch of about 6 us and
-// the partials' way to memory and back. `share`: mean over longest keys of a block; `uneven` blocks (the
+// the partials' way to memory and back. `blocks` count by their keys (equal_blocks); `uneven` ones (the
 // causal rule's, longest first) fill their last round. `cost`:
 // receives the estimated time unsplit over the least. Measured, us at 1, 2, 4, 8, 16 chunks (32 heads, 8 key heads, D = 128): 512 queries behind 16,384
 // keys -, -, 144, 157, 181; 128 behind 16,384 -, -, -, -, 57 (74 at 32); 4 x 64 behind 500 to 9,000 -, -, 62, 46,
 // 57; 8,192 causal at 4 heads 134, 113, 110, 107; two texts of 12 heads at D = 64 41, 48, 45 (3), 51 (5).
-int fwd_chunks(const vc_packedattn_desc* d, int64_t blocks, double rows, double share, bool uneven, double* cost = nullptr) {
+int fwd_chunks(const vc_packedattn_desc* d, double blocks, double rows, bool uneven, double* cost = nullptr) {
   const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
   const double tile_us = d->head_dim == 128 ? 1.8 : 0.9;
   double least = 1e30;
   int best = 1;
   for (int c = 1; c <= std::min(64, std::max(1, ntile / 4)); ++c) {
     const double span = (ntile + c - 1) / c;
-    const double load = blocks * share * c / 512, rounds = uneven ? std::max(load, 1.0) : ceil(load);
+    const double load = blocks * c / 512, rounds = uneven ? std::max(load, 1.0) : ceil(load);
     const double merge = c == 1 ? 0 : (6 + rows * c * (d->head_dim + 2) * 8 / 4e6) / tile_us;
     const double time = rounds * (span + 3) + merge;
     if (time < least * 0.98) {
@@ -146,6 +158,11 @@ int few_chunks(const vc_packedattn_desc* d, int64_t rows, int64_t blocks) {
   }
   return best;
 }
+// Waves of the kernels that join the chunks: one per (query of a slot, head), by the longest slot.
+double merge_waves(const vc_packedattn_desc* d, int64_t rows) {
+  const double blocks = (double)(rows + vcja::kPackedRows - 1) / vcja::kPackedRows;
+  return blocks * vcja::kPackedRows * d->sequences * d->heads;
+}
 FwdPlan fwd_plan(const vc_packedattn_desc* d) {
   const int group = d->heads / d->kv_heads;
   FwdPlan p;
@@ -153,14 +170,14 @@ FwdPlan fwd_plan(const vc_packedattn_desc* d) {
   const int64_t rows = (int64_t)d->max_q * p.pack, bm = vcja::kPackedRows;
   const int64_t blocks = std::min<int64_t>(d->sequences * ((rows + bm - 1) / bm), d->total_q * p.pack / bm + d->sequences) *
                          (d->heads / p.pack);
-  double share = std::min(1.0, (double)d->total_k / ((double)d->sequences * d->max_k));
   const bool uneven = d->causal && 2 * (int64_t)d->max_q > d->max_k;
-  if (uneven) share *= 0.5;
+  const double work = equal_blocks(d, rows, d->total_q * p.pack, d->max_k, d->total_k) * (d->heads / p.pack) * (uneven ? 0.5 : 1.0);
   p.few = rows <= 32;
   const int64_t grid = d->sequences * ((rows + bm - 1) / bm) * (d->heads / p.pack), outs = d->total_q * d->heads;
   const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
-  p.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(p.few ? few_chunks(d, outs, blocks) : fwd_chunks(d, blocks, (double)outs, share, uneven),
+  p.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(p.few ? few_chunks(d, outs, blocks) : fwd_chunks(d, work, (double)outs, uneven),
                                                           kMaxGrid / grid));
+  if (merge_waves(d, rows) > kMaxGrid) p.chunks = 1;
   p.span = (ntile + p.chunks - 1) / p.chunks;
   p.chunks = (ntile + p.span - 1) / p.span;
   return p;
@@ -178,14 +195,13 @@ struct DqPlan {
 };
 DqPlan dq_plan(const vc_packedattn_desc* d) {
   const int64_t bm = vcja::kPackedRows, per = (d->max_q + bm - 1) / bm;
-  const int64_t blocks = std::min<int64_t>(d->sequences * per, d->total_q / bm + d->sequences) * d->heads;
-  double share = std::min(1.0, (double)d->total_k / ((double)d->sequences * d->max_k));
   const bool uneven = d->causal && 2 * (int64_t)d->max_q > d->max_k;
-  if (uneven) share *= 0.5;
+  const double work = equal_blocks(d, d->max_q, d->total_q, d->max_k, d->total_k) * d->heads * (uneven ? 0.5 : 1.0);
   const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
   double gain = 1;
-  int64_t chunks = fwd_chunks(d, blocks, (double)d->total_q * d->heads, share, uneven, &gain);
-  chunks = gain * 0.7 < 1 ? 1 : std::max<int64_t>(1, std::min(chunks, kMaxGrid / (d->sequences * per * d->heads)));
+  int64_t chunks = fwd_chunks(d, work, (double)d->total_q * d->heads, uneven, &gain);
+  chunks = gain * 0.7 < 1 || merge_waves(d, d->max_q) > kMaxGrid
+               ? 1 : std::max<int64_t>(1, std::min(chunks, kMaxGrid / (d->sequences * per * d->heads)));
   DqPlan p;
   p.span = (int)((ntile + chunks - 1) / chunks);
   p.chunks = (ntile + p.span - 1) / p.span;
@@ -207,7 +223,9 @@ size_t stat_bytes(const vc_packedattn_desc* d) {
 // 183; 4 x 4,096 1255 / 1189; 1 x 12,000, 2 key heads 2565 / 2387.
 int key_chunks(const vc_packedattn_desc* d) {
   const int bm = vcja::kPackedRows, group = d->heads / d->kv_heads;
-  const int64_t items = d->kv_heads * std::min<int64_t>((int64_t)d->sequences * ((d->max_k + bm - 1) / bm), d->total_k / bm + d->sequences);
+  // blocks of all slots, but not many more than their work amounts to
+  const int64_t items = d->kv_heads * std::min<int64_t>({(int64_t)d->sequences * ((d->max_k + bm - 1) / bm), d->total_k / bm + d->sequences,
+                                                         (int64_t)(2 * equal_blocks(d, d->max_k, d->total_k, d->max_q, d->total_q)) + 1});
   const int64_t steps = (int64_t)group * ((d->max_q + 31) / 32);
   const int64_t want = std::min((1024 + items - 1) / items, std::max((512 + items - 1) / items, steps / 96));
   const int64_t grid = (int64_t)d->sequences * ((d->max_k + bm - 1) / bm) * d->kv_heads;

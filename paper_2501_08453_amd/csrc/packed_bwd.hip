@@ -87,13 +87,14 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedA
   const int lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hi = lane >> 5;
-  const int blocks = a.nblk * a.H * a.S, items = blocks * a.dq_chunks;
+  const int blocks = a.blocks * a.H, items = blocks * a.dq_chunks;
   if ((int)blockIdx.x >= items) {
     clear_rows<D>(a.dq, nullptr, a.cu_q, a.S, a.Tq, a.H, blockIdx.x - items, gridDim.x - items, tid, 64 * NW);
     return;
   }
   const int chunk = (int)blockIdx.x / blocks;  // of the block's key tiles
-  const PackedItem it = packed_item(blockIdx.x % blocks, a.nblk, a.Hkv, a.G, a.S);
+  const PackedItem it = packed_item(a, blockIdx.x % blocks, a.cu_q, a.Tq, a.Hkv, a.G, true);
+  if (it.s < 0) return;
   const SeqRows sr = seq_rows(a, it.s);
   const int b0 = it.blk * BM;
   if (b0 >= sr.sq) return;
@@ -317,8 +318,20 @@ __global__ __launch_bounds__(256) void packed_dq_sum_kernel(PackedArgs a) {
   typedef float fe __attribute__((ext_vector_type(E)));
   const int lane = threadIdx.x & 63;
   const int x = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
-  if (x >= a.S * a.max_q * a.H) return;
-  const int h = x % a.H, i = x / a.H % a.max_q, s = x / a.H / a.max_q;
+  int h, i, s;
+  if (a.compact) {  // (row of a block, head, block)
+    const int c = x / (kPackedRows * a.H);
+    if (c >= a.blocks) return;
+    s = find_sequence(a.cu_q, a.S, a.Tq, c);
+    if (s < 0) return;
+    i = __builtin_amdgcn_readfirstlane((c - min(max(a.cu_q[s], 0), a.Tq) / kPackedRows - s) * kPackedRows + x % kPackedRows);
+    h = x / kPackedRows % a.H;
+  } else {
+    if (x >= a.S * a.max_q * a.H) return;
+    h = x % a.H;
+    i = x / a.H % a.max_q;
+    s = x / a.H / a.max_q;
+  }
   const SeqRows sr = seq_rows(a, s);
   if (i >= sr.sq) return;
   // The tiles of the row's block of rows, as the dQ kernel counts them.
@@ -382,15 +395,17 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dkdv_kernel(Packe
   const int tid = threadIdx.x;
   const int lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int items = a.nblk * a.Hkv * a.S * a.chunks;
+  const int items = a.blocks * a.Hkv * a.chunks;
   if ((int)blockIdx.x >= items) {
     clear_rows<D>(a.dk, a.dv, a.cu_k, a.S, a.Tk, a.Hkv, blockIdx.x - items, gridDim.x - items, tid, 64 * NW);
     return;
   }
-  // Key heads and sequences run fastest, then the chunks; the first key blocks, the longest
-  // under the causal rule, come first.
-  const int HS = a.Hkv * a.S, kv = blockIdx.x % a.Hkv, seq = blockIdx.x / a.Hkv % a.S;
-  const int chunk = blockIdx.x / HS % a.chunks, blk = blockIdx.x / HS / a.chunks;
+  // Key heads (and sequences) run fastest, the chunks of a block next to each other behind them; the first key
+  // blocks, the longest under the causal rule, come first.
+  const int per = a.compact ? a.Hkv : a.Hkv * a.S, chunk = blockIdx.x / per % a.chunks;
+  const PackedItem it = packed_item(a, blockIdx.x / per / a.chunks * per + blockIdx.x % per, a.cu_k, a.Tk, a.Hkv, 1, false);
+  if (it.s < 0) return;
+  const int kv = it.h, seq = it.s, blk = it.blk;
   const int b0 = blk * BM;
   const SeqRows sr = seq_rows(a, seq);
   if (BIAS && b0 + BM >= sr.sk && (b0 < sr.sk || blk == 0)) {
@@ -760,11 +775,14 @@ namespace {
 template <int D, int RMAX>
 void launch_bwd(PackedArgs a, __bf16* dbias, int clear, hipStream_t s) {
   const dim3 block(64 * kPackedWaves);
-  a.nblk = (a.max_q + kPackedRows - 1) / kPackedRows;
-  hipLaunchKernelGGL((packed_dq_kernel<D, RMAX>), dim3(a.nblk * a.H * a.S * a.dq_chunks + clear), block, 0, s, a);
-  if (a.dq_chunks > 1) hipLaunchKernelGGL(packed_dq_sum_kernel<D>, dim3((a.S * a.max_q * a.H + 3) / 4), dim3(256), 0, s, a);
-  a.nblk = (a.max_k + kPackedRows - 1) / kPackedRows;
-  hipLaunchKernelGGL((packed_dkdv_kernel<D, RMAX>), dim3(a.nblk * a.Hkv * a.S * a.chunks + clear), block, 0, s, a);
+  set_blocks(a, a.max_q, a.Tq);
+  hipLaunchKernelGGL((packed_dq_kernel<D, RMAX>), dim3(a.blocks * a.H * a.dq_chunks + clear), block, 0, s, a);
+  if (a.dq_chunks > 1) {
+    const int waves = a.compact ? a.blocks * a.H * kPackedRows : a.S * a.max_q * a.H;
+    hipLaunchKernelGGL(packed_dq_sum_kernel<D>, dim3((waves + 3) / 4), dim3(256), 0, s, a);
+  }
+  set_blocks(a, a.max_k, a.Tk);
+  hipLaunchKernelGGL((packed_dkdv_kernel<D, RMAX>), dim3(a.blocks * a.Hkv * a.chunks + clear), block, 0, s, a);
   if (a.chunks > 1) {
     const size_t threads = (size_t)a.Tk * a.Hkv * D / 4;
     hipLaunchKernelGGL(packed_key_sum_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, s, a, a.Hkv * D);

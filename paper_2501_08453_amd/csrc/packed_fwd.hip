@@ -116,13 +116,14 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_fwd_kernel(Packed
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, hi = lane >> 5;
   const int gh = a.G / a.pack;  // head blocks of a group
-  const int items = a.nblk * a.Hkv * gh * a.S * a.chunks;
+  const int blocks = a.blocks * a.Hkv * gh, items = blocks * a.chunks;
   if ((int)blockIdx.x >= items) {
     clear_o<D>(a, blockIdx.x - items, gridDim.x - items, tid, 64 * NW);
     return;
   }
-  const int chunk = (int)blockIdx.x / (items / a.chunks);
-  const PackedItem it = packed_item(blockIdx.x % (items / a.chunks), a.nblk, a.Hkv, gh, a.S);
+  const int chunk = (int)blockIdx.x / blocks;
+  const PackedItem it = packed_item(a, blockIdx.x % blocks, a.cu_q, a.Tq, a.Hkv, gh, true);
+  if (it.s < 0) return;
   const SeqRows sr = seq_rows(a, it.s);
   const int b0 = it.blk * BM;
   if (b0 >= sr.sq * a.pack) return;
@@ -574,9 +575,21 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedArgs a) {
   typedef float fe __attribute__((ext_vector_type(E)));
   const int lane = threadIdx.x & 63;
   const int x = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
-  if (x >= a.S * a.max_q * a.H) return;
-  const int h = x % a.H, i = x / a.H % a.max_q;
-  const SeqRows sr = seq_rows(a, x / a.H / a.max_q);
+  int h, i, s;
+  if (a.compact) {  // (row of a block, head, block)
+    const int c = x / (kPackedRows * a.H);
+    if (c >= a.blocks) return;
+    s = find_sequence(a.cu_q, a.S, a.Tq, c);
+    if (s < 0) return;
+    i = __builtin_amdgcn_readfirstlane((c - min(max(a.cu_q[s], 0), a.Tq) / kPackedRows - s) * kPackedRows + x % kPackedRows);
+    h = x / kPackedRows % a.H;
+  } else {
+    if (x >= a.S * a.max_q * a.H) return;
+    h = x % a.H;
+    i = x / a.H % a.max_q;
+    s = x / a.H / a.max_q;
+  }
+  const SeqRows sr = seq_rows(a, s);
   if (i >= sr.sq) return;
   // The keys of the row's block of rows, as the forward counts them.
   const int row = i * a.pack + h % a.pack, b0 = row / kPackedRows * kPackedRows;
@@ -618,13 +631,16 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedArgs a) {
 template <int D, int RMAX>
 void launch(PackedArgs a, hipStream_t s) {
   const int clear = a.clear ? 32 : 0, heads = a.H / a.pack;
+  set_blocks(a, a.pack > 1 ? 1 : a.max_q, a.Tq);  // heads packed into a block: one block a slot
   if (a.few) {
     hipLaunchKernelGGL((packed_few_kernel<D, RMAX>), dim3(heads * a.S * a.chunks + clear), dim3(64 * kFewWaves), 0, s, a);
   } else {
-    a.nblk = (a.max_q * a.pack + kPackedRows - 1) / kPackedRows;
-    hipLaunchKernelGGL((packed_fwd_kernel<D, RMAX>), dim3(a.nblk * heads * a.S * a.chunks + clear), dim3(64 * kPackedWaves), 0, s, a);
+    hipLaunchKernelGGL((packed_fwd_kernel<D, RMAX>), dim3(a.blocks * heads * a.chunks + clear), dim3(64 * kPackedWaves), 0, s, a);
   }
-  if (a.chunks > 1) hipLaunchKernelGGL(packed_merge_kernel<D>, dim3((a.S * a.max_q * a.H + 3) / 4), dim3(256), 0, s, a);
+  if (a.chunks > 1) {
+    const int waves = a.compact ? a.blocks * a.H * kPackedRows : a.S * a.max_q * a.H;
+    hipLaunchKernelGGL(packed_merge_kernel<D>, dim3((waves + 3) / 4), dim3(256), 0, s, a);
+  }
 }
 
 }  // namespace

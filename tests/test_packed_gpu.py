@@ -263,6 +263,19 @@ def test_few_rows_behind_long_caches(lq, H, Hkv, nb, D):
     check(x, d, desc)
 
 
+@pytest.mark.parametrize("D,nb", [(64, 0), (64, 9), (128, 0)])
+@pytest.mark.parametrize("long", [700, 3000])
+def test_one_long_sequence_among_many_short(long, D, nb):
+    """Blocks numbered through and looked up; with the longer one its keys shared by several workgroups."""
+    g = np.random.default_rng(6)
+    lens = [int(n) for n in g.integers(0, 20, 300)]
+    lens[137] = long
+    x, d, desc = make(30, lens, lens, 2, 2, D, True, nb, 30 if nb else 0, outside=(3, 200))
+    check(x, d, desc)
+    more = [min(n, 400) for n in lens]  # and keys before the queries', more than 64 x 64 sequences beside
+    check(*make(31, more + [1] * 4000, [n + 3 for n in more] + [1] * 4000, 2, 1, D, False))
+
+
 def test_reproducible():
     """Two runs agree bitwise."""
     import torch
