@@ -404,7 +404,9 @@ vc_status vc_offload_wait(vc_offload* h, void* stream);
  *   bias, and where the bucket is none of 0 .. num_buckets - 1),
  *
  * and LSE, O, dQ, dK, dV as above (dK, dV summed over the query heads of a group) and
- * dbias[h][u] = the sum of dS_ij over the pairs of bucket u. A query that sees no key
+ * dbias[h][u] = the sum of dS_ij over the pairs of bucket u. Probabilities and sums are
+ * fp32; P and dS are rounded to bf16 for the products with V, K, Q and dO (the matrix cores'
+ * operands). A query that sees no key
  * (causal, and more queries than keys; or shut out by the bias) gets O = 0, LSE = -inf,
  * dQ = 0. An entry of the bias below -65536 (-inf, or a type's lowest value) shuts its
  * pairs out: probability exactly 0; one above 65536 counts as 65536.
@@ -413,15 +415,18 @@ vc_status vc_offload_wait(vc_offload* h, void* stream);
  *    contiguous like q; dk, dv like k. lse: fp32 [heads, total_q].
  *  - cu_q, cu_k: device int32 [S + 1], not decreasing; len_q, len_k: device int32 [S] or
  *    NULL. They are read on the device only: an offset or length outside its tensor or slot
- *    is taken as the nearest inside, a slot of more than max_q (max_k) rows as one of
- *    that many.
+ *    is taken as the nearest inside, and nothing outside the tensors is read or written
+ *    whatever they hold. No slot may have more than max_q (max_k) rows: what stands in the
+ *    outputs for the rows behind is then not defined.
  *  - bias: bf16 [heads, num_buckets]; buckets: device int32 [2 R + 1]. Both NULL or
  *    ignored with num_buckets = 0.
  *  - Rows of a slot behind its length get O = 0, LSE = -inf, dQ = 0 (dK = dV = 0 exactly);
  *    what q, k, v and dout hold there has no effect. Rows outside every slot are left as
  *    they were, or with `clear_outside` written as those. Values of rows that take part must be
  *    finite: a causal query's row is computed together with up to 63 later keys.
- *  - Deterministic: no atomics; dK and dV of a key are summed in one order.
+ *  - Deterministic: no atomics, every sum in one order, which follows from the descriptor and
+ *    the lengths alone (a sequence's results can differ by rounding from those of the same
+ *    sequence in another batch, where keys are shared by other numbers of workgroups).
  * ------------------------------------------------------------------------- */
 typedef struct vc_packedattn_desc {
   int32_t sequences;      /* S >= 1                                             */
@@ -442,8 +447,9 @@ typedef struct vc_packedattn_desc {
   int32_t clear_outside;  /* 1: outputs' rows outside every slot are written too */
 } vc_packedattn_desc;
 
-/* Bytes of device workspace of the forward and of the backward (the backward: per query
- * row and head fp32 -LSE/c and -D, and the bias gradient's sums per distance); 0 for an
+/* Bytes of device workspace of the forward (fp32 partial results where several workgroups
+ * share a row's keys) and of the backward (per query row and head fp32 -LSE/c and -D, the
+ * bias gradient's sums per distance, partial dQ or dK and dV where work is shared); 0 for an
  * invalid descriptor. Host only. */
 size_t vc_packedattn_fwd_workspace_bytes(const vc_packedattn_desc* desc);
 size_t vc_packedattn_bwd_workspace_bytes(const vc_packedattn_desc* desc);

@@ -61,11 +61,12 @@ def vc_layernorm_bwd(desc, dout, x, weight, mean, rstd, dx, dweight, dbias, work
 
 def make_packed_desc(sequences, heads, kv_heads, head_dim, total_q, total_k, max_q, max_k, causal=False, scale=None,
                      num_buckets=0, max_distance=0):
-    """Descriptor of a packed call: `sequences` slots in total_q query rows and total_k key rows, the longest of
-    max_q and max_k rows (upper bounds are enough; a longer slot is cut). With num_buckets, every call takes a
+    """Descriptor of a packed call: `sequences` slots in total_q query rows and total_k key rows, none of more than
+    max_q and max_k rows (upper bounds are enough, exact ones give the best division of the work). With num_buckets, every call takes a
     bias [heads, num_buckets] and the buckets of the distances -max_distance .. max_distance."""
-    return vc_packedattn_desc(int(sequences), int(heads), int(kv_heads), int(head_dim), int(total_q), int(total_k), int(max_q),
-                              int(max_k), 0, 0, 0, 1 if causal else 0, float(scale) if scale else 0.0, int(num_buckets),
+    return vc_packedattn_desc(int(sequences), int(heads), int(kv_heads), int(head_dim), int(total_q), int(total_k),
+                              min(int(max_q), int(total_q)), min(int(max_k), int(total_k)), 0, 0, 0, 1 if causal else 0,
+                              float(scale) if scale else 0.0, int(num_buckets),
                               int(max_distance), 0)
 
 
@@ -333,7 +334,8 @@ def _autograd_functions():
 
 
 def packed_attention(q, k, v, desc, cu_q, cu_k, len_q=None, len_k=None, bias=None, buckets=None):
-    """Differentiable packed attention (see packed_fwd): gradients of q, k, v and the bias."""
+    """Differentiable packed attention (see packed_fwd): gradients of q, k, v and the bias. For a captured graph take
+    packed_fwd and packed_bwd: autograd itself waits, across streams, for other graphs of the same leaves."""
     return _autograd_functions()["packed"].apply(q, k, v, bias, desc, cu_q, cu_k, len_q, len_k, buckets)
 
 
