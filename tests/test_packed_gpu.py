@@ -347,3 +347,42 @@ def test_differentiable_form():
     assert torch.equal(qkv.grad, torch.cat([want["dq"], want["dk"], want["dv"]], 1))
     frozen = vc.packed_attention(qkv[:, :4], qkv[:, 4:6], qkv[:, 6:], desc, d["cu_q"], d["cu_k"], bias=d["bias"], buckets=d["buckets"])
     assert torch.equal(torch.autograd.grad(frozen, qkv, d["dout"])[0], qkv.grad)
+
+
+def test_offsets_past_32_bits():
+    """Slots whose rows start behind 2^31 elements of every tensor: a second sequence of 70 queries and 130 keys there, 3 rows
+    of each in the first one's long slot."""
+    import torch
+    vc = _vc()
+    H, D, n = 32, 128, 560_000
+    assert (n - 1000) * H * D > 2 ** 31
+    g = torch.Generator().manual_seed(40)
+    cu = torch.tensor([0, n - 1000, n], dtype=torch.int32).cuda()
+    lens = {"q": [3, 70], "k": [3, 130]}
+    big = {m: torch.empty((n, H, D), dtype=torch.bfloat16, device="cuda") for m in ("q", "k", "v", "dout")}
+    small = {}
+    for m, t in big.items():
+        a, b = lens["q" if m in ("q", "dout") else "k"]
+        small[m] = torch.randn((a + b, H, D), generator=g).to(torch.bfloat16)
+        t[:a] = small[m][:a].cuda()
+        t[n - 1000:n - 1000 + b] = small[m][a:].cuda()
+    desc = vc.make_packed_desc(2, H, H, D, n, n, n - 1000, n - 1000, causal=True)
+    kw = {"len_q": torch.tensor(lens["q"], dtype=torch.int32).cuda(), "len_k": torch.tensor(lens["k"], dtype=torch.int32).cuda()}
+    o, lse = vc.packed_fwd(big["q"], big["k"], big["v"], desc, cu, cu, **kw)
+    dq, dk, dv, _ = vc.packed_bwd(big["q"], big["k"], big["v"], o, lse, big["dout"], desc, cu, cu, **kw)
+    x = {m: t.double().numpy() for m, t in small.items()}
+    x.update(cu_q=np.array([0, 3, 73]), cu_k=np.array([0, 3, 133]), len_q=None, len_k=None, causal=True, scale=None)
+    r, tol = bounds(x, 2 * lse_bound(x, D, 130, 1 / np.sqrt(D), np.zeros(1)) + 2.0 ** -20)
+    for m, t in (("o", o), ("dq", dq), ("dk", dk), ("dv", dv)):
+        a, b = lens["q" if m in ("o", "dq") else "k"]
+        got = bf16_values(torch.cat([t[:a], t[n - 1000:n - 1000 + b]]))
+        off = float((np.abs(got - r[m]) / tol[m]).max())
+        log("   %-3s off / bound %.3f" % (m, off))
+        assert off <= 1, m
+        assert not t[a:n - 1000].any() and not t[n - 1000 + b:].any(), m  # rows of the slots behind their lengths
+    # one token each at the end of the same caches
+    one = vc.make_packed_desc(2, H, H, D, 2, n, 1, n - 1000, causal=True)
+    ends = torch.tensor([0, 1, 2], dtype=torch.int32).cuda()
+    o1, _ = vc.packed_fwd(torch.cat([big["q"][2:3], big["q"][n - 1000 + 69:n - 1000 + 70]]), big["k"], big["v"], one, ends, cu, len_k=kw["len_k"])
+    got, last = bf16_values(o1), [2, 72]
+    assert (np.abs(got - r["o"][last]) <= tol["o"][last]).all()
