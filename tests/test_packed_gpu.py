@@ -276,6 +276,26 @@ def test_one_long_sequence_among_many_short(long, D, nb):
     check(*make(31, more + [1] * 4000, [n + 3 for n in more] + [1] * 4000, 2, 1, D, False))
 
 
+@pytest.mark.parametrize("D,nb", [(64, 0), (64, 12), (128, 0)])
+def test_few_keys_of_unequal_weight(D, nb):
+    """Gradients of texts of a few tokens, where dS is much smaller than D = <dO, O>: dQ and dK are off (2-norm) by no more
+    than two roundings to bf16 (dS and the result: relative rms at most 2^-8 / sqrt(3) each, where a value stands
+    at the bottom of its binade), 2^-8 sqrt(2 / 3) = 0.0032, and 0.0003 for the fp32 part; not by the rounding of O in D."""
+    lens = [n for n in range(2, 7)] * 20
+    for causal in (False, True):
+        x, d, desc = make(33, lens, lens, 2, 2, D, causal, nb, 4 if nb else 0)
+        x["bias"] = x["bias"] * 2 if nb else None  # logits of a spread of 2 and more
+        if nb:
+            d["bias"] = d["bias"] * 2
+        out = run(d, desc)
+        r = T.packed_attention(**{n: x[n] for n in ("q", "k", "v", "dout", "cu_q", "cu_k", "causal") if n in x},
+                               bias=x["bias"], buckets=x.get("buckets"))
+        for n in ("dq", "dk"):
+            off = np.linalg.norm(bf16_values(out[n]) - r[n]) / np.linalg.norm(r[n])
+            log("   %s %.4f" % (n, off))
+            assert off <= 0.0035, n
+
+
 def test_reproducible():
     """Two runs agree bitwise."""
     import torch
