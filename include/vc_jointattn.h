@@ -31,7 +31,7 @@
  * a joint permutation of keys and values), so the paper's interleaving of text
  * and visual embeddings is an ordering choice the caller may make freely.
  *
- * Conventions for every entry point
+ * Conventions for every entry point (the text tower's, at the end, have layouts of their own)
  *  - Tensors q, k, v, o, dout, dq, dk, dv: bf16, contiguous [B, N, H, D]
  *    (head_dim fastest), device memory, 16-byte aligned.
  *  - lse: fp32 [B, H, N], device memory, 16-byte aligned.

@@ -10,6 +10,10 @@
 //   of the group, so that dK and dV of the shared head are summed in registers; where that leaves
 //   too few workgroups, each takes a run of those tiles and fp32 partials are summed afterwards.
 //   With a bias it also sums dS over every distance, in LDS.
+// Both are bound by the matrix rate for long rows: 12,000 tokens causal, 16 heads, 2 key heads, D = 128: dQ 783 us,
+// 1,130 TFLOP/s of its 6 D a pair, dK/dV 1,135 us, 1,039 of 8 D (the first, plain walks, operands read where they
+// are used and the statistics from memory: 6.5 ms for forward and backward, now 2.4). Short ones wait for a few
+// tiles one after the other: captions of 8 to 256 tokens, 16 heads, D = 64, bias, 23 and 30 us.
 // No atomics anywhere: results are bitwise reproducible.
 #include "packed.hpp"
 
@@ -751,7 +755,8 @@ __global__ __launch_bounds__(256) void packed_key_sum_kernel(PackedArgs a, int p
 
 // Bias gradient, one workgroup per head: the blocks' sums per distance added up in order, then
 // the distances of each bucket. In both steps the threads share the sums of one result by runs,
-// which are then joined in order.
+// which are then joined in order (one thread per result, bounds looked up at each block: 28 us for
+// captions of 8 to 256 tokens at 16 heads, so 6).
 __global__ __launch_bounds__(1024) void packed_dbias_kernel(PackedArgs a, __bf16* dbias) {
   __shared__ float part[1024];
   __shared__ float sum[2 * kMaxBiasDistance + 1];
