@@ -7,6 +7,7 @@ every step of the computation runs in the library's HIP kernels (include/vc_join
 from __future__ import annotations
 
 import ctypes
+import math
 
 from paper_2501_08453_amd import (_call, _check_placed, _check_shape, _lib, _ptr, _stream, _workspace,
                                   vc_layernorm_desc, vc_packedattn_desc)
@@ -183,13 +184,18 @@ def packed_fwd(q, k, v, desc, cu_q, cu_k, len_q=None, len_k=None, bias=None, buc
     """(o, lse) of packed attention: q [total_q, heads, D], k and v [total_k, kv_heads, D] in bf16 (tokens may be any
     multiple of 8 elements apart, as in slices of one projection), lse [heads, total_q]. Sequence s has the rows
     [cu_q[s], cu_q[s+1]) and [cu_k[s], cu_k[s+1]) or, of these, the first len_q[s] and len_k[s]. Rows outside every
-    slot are 0 (lse -inf) in tensors made here, and left as they were where `out` is given."""
+    slot are 0 (lse: -inf) in each tensor made here, and left as they were in `out` or `lse` where that is given."""
     import torch
-    made = out is None
-    out = torch.empty((desc.total_q, desc.heads, desc.head_dim), dtype=torch.bfloat16, device=q.device) if made else out
-    lse = torch.empty((desc.heads, desc.total_q), dtype=torch.float32, device=q.device) if lse is None else lse
+    clear = out is None and lse is None  # by the library: both; where one is given, the other is filled beforehand
+    if out is None:
+        new = torch.empty if clear else torch.zeros
+        out = new((desc.total_q, desc.heads, desc.head_dim), dtype=torch.bfloat16, device=q.device)
+    if lse is None:
+        shape = (desc.heads, desc.total_q)
+        lse = (torch.empty(shape, dtype=torch.float32, device=q.device) if clear
+               else torch.full(shape, -math.inf, dtype=torch.float32, device=q.device))
     d = _check_packed(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets, (("out", out),), (), lse)
-    d.clear_outside = 1 if made else 0
+    d.clear_outside = 1 if clear else 0
     ws = packed_fwd_workspace(d, q.device) if ws is None else ws
     _launch(q.device, vc_packedattn_fwd, d, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets, out, lse, ws, ws.numel())
     return out, lse

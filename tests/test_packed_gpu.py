@@ -406,3 +406,24 @@ def test_offsets_past_32_bits():
     o1, _ = vc.packed_fwd(torch.cat([big["q"][2:3], big["q"][n - 1000 + 69:n - 1000 + 70]]), big["k"], big["v"], one, ends, cu, len_k=kw["len_k"])
     got, last = bf16_values(o1), [2, 72]
     assert (np.abs(got - r["o"][last]) <= tol["o"][last]).all()
+
+
+@pytest.mark.parametrize("given", ["out", "lse"])
+def test_one_output_given(given):
+    """Rows before the first and behind the last slot: left as they were in the output that is given, 0 (lse: -inf) in the one
+    that is not, whatever its memory held before."""
+    import torch
+    vc = _vc()
+    x, d, desc = make(41, [20, 0, 65], [30, 4, 65], 4, 2, 64, True, slack=(7, 0), outside=(5, 9))
+    want = dict(zip(("out", "lse"), vc.packed_fwd(d["q"], d["k"], d["v"], desc, d["cu_q"], d["cu_k"], **_kw(d))))
+    kept = torch.full_like(want[given], 7.0)
+    torch.cuda.synchronize()
+    used = [torch.full_like(t, 3.0) for t in want.values() for _ in range(4)]  # what the allocator hands out next
+    del used
+    got = dict(zip(("out", "lse"), vc.packed_fwd(d["q"], d["k"], d["v"], desc, d["cu_q"], d["cu_k"], **{given: kept}, **_kw(d))))
+    assert got[given] is kept
+    a, b = int(x["cu_q"][0]), int(x["cu_q"][-1])
+    for n, t in got.items():
+        rows, ref = (t.t(), want[n].t()) if n == "lse" else (t, want[n])
+        assert torch.equal(rows[a:b], ref[a:b]), n
+        assert all((r == 7).all() if n == given else torch.equal(r, f) for r, f in ((rows[:a], ref[:a]), (rows[b:], ref[b:]))), n
