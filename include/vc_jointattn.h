@@ -62,7 +62,7 @@ extern "C" {
 /* Raised with every change of a signature, a struct, the meaning of an argument or a
  * documented result; the Python binding refuses a library that reports another
  * version. */
-#define VC_JOINTATTN_ABI_VERSION 12
+#define VC_JOINTATTN_ABI_VERSION 13
 
 typedef enum vc_status {
   VC_OK = 0,
@@ -450,7 +450,9 @@ typedef struct vc_packedattn_desc {
 /* Bytes of device workspace of the forward (fp32 partial results where several workgroups
  * share a row's keys) and of the backward (per query row and head fp32 -LSE/c and -D, the
  * bias gradient's sums per distance, partial dQ or dK and dV where work is shared); 0 for an
- * invalid descriptor. Host only. */
+ * invalid descriptor, and where a launch of the call would take 2^32 threads or more (blocks of
+ * 128 rows x heads, or sequences x heads of single tokens, from about 2^24 on), which the call
+ * refuses with VC_ERR_SHAPE. Host only. */
 size_t vc_packedattn_fwd_workspace_bytes(const vc_packedattn_desc* desc);
 size_t vc_packedattn_bwd_workspace_bytes(const vc_packedattn_desc* desc);
 
@@ -490,7 +492,7 @@ vc_status vc_packedattn_bwd(const vc_packedattn_desc* desc,
 #define VC_FP32 1
 
 typedef struct vc_layernorm_desc {
-  int64_t rows;           /* 1 .. 2^30                                          */
+  int64_t rows;           /* 1 .. 2^30; beyond 8,192 columns below 2^24         */
   int32_t cols;           /* 1 .. 65536                                         */
   int32_t x_type;         /* VC_BF16 or VC_FP32: x, y, dout, dx                 */
   int32_t param_type;     /* VC_BF16 or VC_FP32: weight, bias and their gradients */

@@ -17,7 +17,10 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 inline const __bf16* bf(const void* p) { return static_cast<const __bf16*>(p); }
 
-constexpr int64_t kMaxGrid = (int64_t)1 << 30;    // workgroups of one launch, waves of a merge
+// A launch takes less than 2^32 threads: workgroups of 256 beside those that clear, waves of a merge.
+constexpr int64_t kMaxGroups = (((int64_t)1 << 32) - 1) / 256;
+constexpr int64_t kMaxGrid = kMaxGroups - vcja::kClearGroups;
+constexpr int64_t kMaxWaves = 4 * kMaxGroups;
 constexpr int64_t kMaxRows = (int64_t)1 << 30;
 constexpr int64_t kMaxStride = (int64_t)1 << 23;  // elements between tokens: tile offsets of 16 rows stay in 32 bits
 
@@ -105,7 +108,7 @@ double equal_blocks(const vc_packedattn_desc* d, int64_t longest, int64_t total,
 // Forward: heads of a group packed into a row block, and the chunks of a row block's key tiles.
 struct FwdPlan {
   int pack, chunks, span;
-  bool few;
+  bool few, fits;  // fits: the launches can be made
 };
 // The chunks of least estimated time, in tiles of 64 keys x 128 rows (about 1.8 us at head_dim 128, half
 // of that at 64, with two workgroups a compute unit): rounds over 512 places, each workgroup 3 tiles
@@ -158,10 +161,15 @@ int few_chunks(const vc_packedattn_desc* d, int64_t rows, int64_t blocks) {
   }
   return best;
 }
-// Waves of the kernels that join the chunks: one per (query of a slot, head), by the longest slot.
-double merge_waves(const vc_packedattn_desc* d, int64_t rows) {
-  const double blocks = (double)(rows + vcja::kPackedRows - 1) / vcja::kPackedRows;
-  return blocks * vcja::kPackedRows * d->sequences * d->heads;
+vcja::RowBlocks query_blocks(const vc_packedattn_desc* d, int pack) {  // heads packed into a block: one block a slot
+  return vcja::row_blocks(pack > 1 ? 1 : d->max_q, d->total_q, d->sequences, d->kv_heads);
+}
+vcja::RowBlocks key_blocks(const vc_packedattn_desc* d) {
+  return vcja::row_blocks(d->max_k, d->total_k, d->sequences, d->kv_heads);
+}
+// Waves of the kernels that join the chunks: one per (query of a slot, head).
+int64_t merge_waves(const vc_packedattn_desc* d, const vcja::RowBlocks& b) {
+  return (b.compact ? b.blocks * vcja::kPackedRows : (int64_t)d->sequences * d->max_q) * d->heads;
 }
 FwdPlan fwd_plan(const vc_packedattn_desc* d) {
   const int group = d->heads / d->kv_heads;
@@ -173,17 +181,18 @@ FwdPlan fwd_plan(const vc_packedattn_desc* d) {
   const bool uneven = d->causal && 2 * (int64_t)d->max_q > d->max_k;
   const double work = equal_blocks(d, rows, d->total_q * p.pack, d->max_k, d->total_k) * (d->heads / p.pack) * (uneven ? 0.5 : 1.0);
   p.few = rows <= 32;
-  const int64_t grid = d->sequences * ((rows + bm - 1) / bm) * (d->heads / p.pack), outs = d->total_q * d->heads;
+  const vcja::RowBlocks b = query_blocks(d, p.pack);
+  const int64_t grid = (p.few ? d->sequences : b.blocks) * (d->heads / p.pack), outs = d->total_q * d->heads;
   const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
   p.chunks = (int)std::max<int64_t>(1, std::min<int64_t>(p.few ? few_chunks(d, outs, blocks) : fwd_chunks(d, work, (double)outs, uneven),
                                                           kMaxGrid / grid));
-  if (merge_waves(d, rows) > kMaxGrid) p.chunks = 1;
+  if (merge_waves(d, b) > kMaxWaves) p.chunks = 1;
+  p.fits = grid <= kMaxGrid;
   p.span = (ntile + p.chunks - 1) / p.chunks;
   p.chunks = (ntile + p.span - 1) / p.span;
   return p;
 }
-size_t fwd_part_bytes(const vc_packedattn_desc* d) {
-  const FwdPlan p = fwd_plan(d);
+size_t fwd_part_bytes(const vc_packedattn_desc* d, const FwdPlan& p) {
   return p.chunks == 1 ? 256 : align256((size_t)p.chunks * d->total_q * d->heads * (d->head_dim + 2) * sizeof(float));
 }
 
@@ -192,23 +201,24 @@ size_t fwd_part_bytes(const vc_packedattn_desc* d) {
 // and 200 of 8,000 and 3,000 324 / 253, 8,192 causal at 4 heads 435 / 420; not so 2,048 causal 159 / 168, 4,096 389 / 410.
 struct DqPlan {
   int chunks, span;
+  bool fits;
 };
 DqPlan dq_plan(const vc_packedattn_desc* d) {
-  const int64_t bm = vcja::kPackedRows, per = (d->max_q + bm - 1) / bm;
+  const vcja::RowBlocks b = query_blocks(d, 1);
+  const int64_t grid = b.blocks * d->heads;
   const bool uneven = d->causal && 2 * (int64_t)d->max_q > d->max_k;
   const double work = equal_blocks(d, d->max_q, d->total_q, d->max_k, d->total_k) * d->heads * (uneven ? 0.5 : 1.0);
   const int ntile = (d->max_k + vcja::kTileTok - 1) / vcja::kTileTok;
   double gain = 1;
   int64_t chunks = fwd_chunks(d, work, (double)d->total_q * d->heads, uneven, &gain);
-  chunks = gain * 0.7 < 1 || merge_waves(d, d->max_q) > kMaxGrid
-               ? 1 : std::max<int64_t>(1, std::min(chunks, kMaxGrid / (d->sequences * per * d->heads)));
+  chunks = gain * 0.7 < 1 || merge_waves(d, b) > kMaxWaves ? 1 : std::max<int64_t>(1, std::min(chunks, kMaxGrid / grid));
   DqPlan p;
+  p.fits = grid <= kMaxGrid;
   p.span = (int)((ntile + chunks - 1) / chunks);
   p.chunks = (ntile + p.span - 1) / p.span;
   return p;
 }
-size_t dq_part_bytes(const vc_packedattn_desc* d) {
-  const int c = dq_plan(d).chunks;
+size_t dq_part_bytes(const vc_packedattn_desc* d, int c) {
   return c == 1 ? 0 : align256((size_t)c * d->total_q * d->heads * (d->head_dim + 1) * sizeof(float));
 }
 
@@ -228,25 +238,44 @@ int key_chunks(const vc_packedattn_desc* d) {
                                                          (int64_t)(2 * equal_blocks(d, d->max_k, d->total_k, d->max_q, d->total_q)) + 1});
   const int64_t steps = (int64_t)group * ((d->max_q + 31) / 32);
   const int64_t want = std::min((1024 + items - 1) / items, std::max((512 + items - 1) / items, steps / 96));
-  const int64_t grid = (int64_t)d->sequences * ((d->max_k + bm - 1) / bm) * d->kv_heads;
-  const int64_t chunks = std::max<int64_t>(1, std::min({want, steps / 8, kMaxGrid / grid}));
-  return (int)(d->num_buckets ? (chunks + group - 1) / group * group : chunks);  // with a bias none of two heads
+  // the workgroups of a launch, and the threads of the sum over the chunks (one per 4 elements)
+  const int64_t grid = key_blocks(d).blocks * d->kv_heads;
+  const int64_t most = (d->total_k * d->kv_heads * d->head_dim / 4 + 255) / 256 > kMaxGroups ? 1 : kMaxGrid / grid;
+  const int64_t chunks = std::max<int64_t>(1, std::min({want, steps / 8, most}));
+  if (!d->num_buckets) return (int)chunks;
+  const int64_t whole = (chunks + group - 1) / group * group;  // with a bias none of two heads
+  return (int)(whole <= most ? whole : std::max<int64_t>(group, most / group * group));
 }
-size_t dist_bytes(const vc_packedattn_desc* d) {
+bool key_fits(const vc_packedattn_desc* d, int chunks) {
+  return key_blocks(d).blocks * d->kv_heads * chunks <= kMaxGrid &&
+         (chunks == 1 || (d->total_k * d->kv_heads * d->head_dim / 4 + 255) / 256 <= kMaxGroups);
+}
+struct BwdPlan {
+  DqPlan dq;
+  int key_chunks;
+  bool fits;
+};
+BwdPlan bwd_plan(const vc_packedattn_desc* d) {
+  BwdPlan p;
+  p.dq = dq_plan(d);
+  p.key_chunks = key_chunks(d);
+  p.fits = p.dq.fits && key_fits(d, p.key_chunks);
+  return p;
+}
+size_t dist_bytes(const vc_packedattn_desc* d, int chunks) {
   if (!d->num_buckets) return 0;
   const int bm = vcja::kPackedRows;
-  const int per_head = key_chunks(d) / (d->heads / d->kv_heads);
+  const int per_head = chunks / (d->heads / d->kv_heads);
   return align256((size_t)(vcja::dist_row(d->total_k, d->sequences, 0, bm) + 1) * per_head * d->heads * (2 * d->max_distance + 1) *
                   sizeof(float));
 }
-size_t key_part_bytes(const vc_packedattn_desc* d) {
-  const int c = key_chunks(d);
+size_t key_part_bytes(const vc_packedattn_desc* d, int c) {
   return c == 1 ? 0 : align256((size_t)c * 2 * d->total_k * d->kv_heads * d->head_dim * sizeof(float));
 }
 
 // The partial results of the two passes take the same room, one after the other.
-size_t bwd_ws_bytes(const vc_packedattn_desc* d) {
-  return 2 * stat_bytes(d) + dist_bytes(d) + std::max(key_part_bytes(d), dq_part_bytes(d));
+size_t bwd_ws_bytes(const vc_packedattn_desc* d, const BwdPlan& p) {
+  return 2 * stat_bytes(d) + dist_bytes(d, p.key_chunks) + std::max(key_part_bytes(d, p.key_chunks), dq_part_bytes(d, p.dq.chunks));
 }
 
 vc_status check_inputs(const vc_packedattn_desc* d, const void* q, const void* k, const void* v, const int32_t* cu_q,
@@ -257,6 +286,20 @@ vc_status check_inputs(const vc_packedattn_desc* d, const void* q, const void* k
       !aligned4(len_k) || (d->num_buckets && ((reinterpret_cast<uintptr_t>(bias) & 1u) || !aligned4(buckets))))
     return VC_ERR_ALIGN;
   return VC_OK;
+}
+
+// The descriptor, and whether the launches of the call can be made; fills the plan.
+vc_status check_fwd(const vc_packedattn_desc* d, FwdPlan* p) {
+  const vc_status st = check_packed(d);
+  if (st != VC_OK) return st;
+  *p = fwd_plan(d);
+  return p->fits ? VC_OK : VC_ERR_SHAPE;
+}
+vc_status check_bwd(const vc_packedattn_desc* d, BwdPlan* p) {
+  const vc_status st = check_packed(d);
+  if (st != VC_OK) return st;
+  *p = bwd_plan(d);
+  return p->fits ? VC_OK : VC_ERR_SHAPE;
 }
 
 vc_status check_ws(const void* ws, size_t have, size_t need) {
@@ -270,24 +313,25 @@ vc_status check_ws(const void* ws, size_t have, size_t need) {
 extern "C" {
 
 size_t vc_packedattn_fwd_workspace_bytes(const vc_packedattn_desc* desc) {
-  return check_packed(desc) == VC_OK ? fwd_part_bytes(desc) : 0;
+  FwdPlan p;
+  return check_fwd(desc, &p) == VC_OK ? fwd_part_bytes(desc, p) : 0;
 }
 
 vc_status vc_packedattn_fwd(const vc_packedattn_desc* desc, const void* q, const void* k, const void* v,
                             const int32_t* cu_q, const int32_t* cu_k, const int32_t* len_q, const int32_t* len_k,
                             const void* bias, const int32_t* buckets, void* o, float* lse, void* workspace,
                             size_t workspace_bytes, void* stream) {
-  vc_status st = check_packed(desc);
+  FwdPlan p;
+  vc_status st = check_fwd(desc, &p);
   if (st != VC_OK) return st;
   if (!o || !lse) return VC_ERR_NULL;
   if ((st = check_inputs(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets)) != VC_OK) return st;
   if (!aligned16(o) || !aligned4(lse)) return VC_ERR_ALIGN;
-  if ((st = check_ws(workspace, workspace_bytes, vc_packedattn_fwd_workspace_bytes(desc))) != VC_OK) return st;
+  if ((st = check_ws(workspace, workspace_bytes, fwd_part_bytes(desc, p))) != VC_OK) return st;
   if ((st = vcja::check_device()) != VC_OK) return st;
   vcja::PackedArgs a = packed_args(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets);
   a.o = static_cast<__bf16*>(o);
   a.lse = lse;
-  const FwdPlan p = fwd_plan(desc);
   a.pack = p.pack;
   a.few = p.few;
   a.chunks = p.chunks;
@@ -297,14 +341,16 @@ vc_status vc_packedattn_fwd(const vc_packedattn_desc* desc, const void* q, const
 }
 
 size_t vc_packedattn_bwd_workspace_bytes(const vc_packedattn_desc* desc) {
-  return check_packed(desc) == VC_OK ? bwd_ws_bytes(desc) : 0;
+  BwdPlan p;
+  return check_bwd(desc, &p) == VC_OK ? bwd_ws_bytes(desc, p) : 0;
 }
 
 vc_status vc_packedattn_bwd(const vc_packedattn_desc* desc, const void* q, const void* k, const void* v, const void* o,
                             const float* lse, const void* dout, const int32_t* cu_q, const int32_t* cu_k,
                             const int32_t* len_q, const int32_t* len_k, const void* bias, const int32_t* buckets, void* dq,
                             void* dk, void* dv, void* dbias, void* workspace, size_t workspace_bytes, void* stream) {
-  vc_status st = check_packed(desc);
+  BwdPlan p;
+  vc_status st = check_bwd(desc, &p);
   if (st != VC_OK) return st;
   if (!o || !lse || !dout || !dq || !dk || !dv) return VC_ERR_NULL;
   if ((st = check_inputs(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets)) != VC_OK) return st;
@@ -312,7 +358,7 @@ vc_status vc_packedattn_bwd(const vc_packedattn_desc* desc, const void* q, const
       (reinterpret_cast<uintptr_t>(dbias) & 1u))
     return VC_ERR_ALIGN;
   if (dbias && !desc->num_buckets) return VC_ERR_SHAPE;
-  if ((st = check_ws(workspace, workspace_bytes, vc_packedattn_bwd_workspace_bytes(desc))) != VC_OK) return st;
+  if ((st = check_ws(workspace, workspace_bytes, bwd_ws_bytes(desc, p))) != VC_OK) return st;
   if ((st = vcja::check_device()) != VC_OK) return st;
   vcja::PackedArgs a = packed_args(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets);
   a.o_in = bf(o);
@@ -325,12 +371,11 @@ vc_status vc_packedattn_bwd(const vc_packedattn_desc* desc, const void* q, const
   a.nls = reinterpret_cast<float*>(ws);
   a.dd = reinterpret_cast<float*>(ws + stat_bytes(desc));
   a.dist_part = reinterpret_cast<float*>(ws + 2 * stat_bytes(desc));
-  a.key_part = reinterpret_cast<float*>(ws + 2 * stat_bytes(desc) + dist_bytes(desc));
+  a.key_part = reinterpret_cast<float*>(ws + 2 * stat_bytes(desc) + dist_bytes(desc, p.key_chunks));
   a.part = a.key_part;
-  a.chunks = key_chunks(desc);
-  const DqPlan p = dq_plan(desc);
-  a.dq_chunks = p.chunks;
-  a.span = p.span;
+  a.chunks = p.key_chunks;
+  a.dq_chunks = p.dq.chunks;
+  a.span = p.dq.span;
   return vcja::launch_packed_bwd(a, desc->head_dim, static_cast<__bf16*>(dbias), as_stream(stream)) == hipSuccess ? VC_OK
                                                                                                             : VC_ERR_HIP;
 }
@@ -341,7 +386,7 @@ namespace {
 
 vc_status check_norm(const vc_layernorm_desc* d) {
   if (!d) return VC_ERR_NULL;
-  if (d->rows < 1 || d->rows > kMaxRows || d->cols < 1 || d->cols > (1 << 16)) return VC_ERR_SHAPE;
+  if (d->rows < 1 || d->cols < 1 || d->cols > (1 << 16) || d->rows > vcja::norm_max_rows(d->cols)) return VC_ERR_SHAPE;
   for (const int t : {d->x_type, d->param_type})
     if (t != VC_BF16 && t != VC_FP32) return VC_ERR_UNSUPPORTED;
   for (const int64_t s : {d->x_stride, d->dout_stride})

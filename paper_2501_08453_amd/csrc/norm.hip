@@ -394,6 +394,8 @@ int row_groups(int64_t rows, int cols, bool backward) {
 
 }  // namespace
 
+int64_t norm_max_rows(int cols) { return cols > kBlockCols ? (((int64_t)1 << 32) - 1) / kThreads : (int64_t)1 << 30; }
+
 int norm_groups(int64_t rows, int cols) {
   if (cols > kBlockCols) return (int)std::max<int64_t>(1, std::min<int64_t>(256, rows / 16));
   return row_groups(rows, cols, true);

@@ -23,6 +23,8 @@ struct NormArgs {
 };
 hipError_t launch_norm_fwd(const NormArgs& a, hipStream_t s);
 hipError_t launch_norm_bwd(const NormArgs& a, hipStream_t s);
+// Most rows of a call (2^30; rows too wide for registers take a workgroup each, and a launch less than 2^32 threads).
+int64_t norm_max_rows(int cols);
 // Runs of rows of the backward's column sums.
 int norm_groups(int64_t rows, int cols);
 

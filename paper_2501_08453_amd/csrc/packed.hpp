@@ -187,14 +187,27 @@ __device__ __forceinline__ int bias_side(int k0, int k1, int p0, int p1, int R) 
 
 // Host-side launchers.
 namespace vcja {
-// The row blocks of a grid over slots of at most `longest` tokens, `total` in all. A search of the sequence is
+// The row blocks of a grid over S slots of at most `longest` tokens, `total` in all. A search of the sequence is
 // worth its time where it saves half of the workgroups and more than a round of them.
-inline void set_blocks(PackedArgs& a, int64_t longest, int64_t total) {
-  a.nblk = (int)((longest + kPackedRows - 1) / kPackedRows);
-  const int64_t all = (int64_t)a.nblk * a.S, through = packed_blocks(total, a.S);
-  a.compact = all > 2 * through && (all - through) * a.Hkv > 1024;
-  a.blocks = (int)(a.compact ? through : all);
+struct RowBlocks {
+  int64_t longest, blocks;  // of the longest slot; of all slots in the grid
+  bool compact;             // numbered through
+};
+inline RowBlocks row_blocks(int64_t longest, int64_t total, int64_t S, int64_t Hkv) {
+  RowBlocks r;
+  r.longest = (longest + kPackedRows - 1) / kPackedRows;
+  const int64_t all = r.longest * S, through = packed_blocks(total, S);
+  r.compact = all > 2 * through && (all - through) * Hkv > 1024;
+  r.blocks = r.compact ? through : all;
+  return r;
 }
+inline void set_blocks(PackedArgs& a, int64_t longest, int64_t total) {
+  const RowBlocks r = row_blocks(longest, total, a.S, a.Hkv);
+  a.nblk = (int)r.longest;
+  a.compact = r.compact;
+  a.blocks = (int)r.blocks;
+}
+constexpr int kClearGroups = 32;  // workgroups of a grid that clear the rows outside every slot
 hipError_t launch_packed_fwd(const PackedArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_packed_bwd(const PackedArgs& a, int head_dim, __bf16* dbias, hipStream_t s);
 }  // namespace vcja

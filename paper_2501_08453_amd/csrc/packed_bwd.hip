@@ -826,7 +826,7 @@ void launch_bwd(PackedArgs a, __bf16* dbias, int clear, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_packed_bwd(const PackedArgs& a, int head_dim, __bf16* dbias, hipStream_t s) {
-  const int clear = a.clear ? 32 : 0;
+  const int clear = a.clear ? kClearGroups : 0;
   const int rmax = !a.bias ? 0 : a.R <= kSmallBiasDistance ? kSmallBiasDistance : kMaxBiasDistance;
   if (head_dim == 128 && rmax == 0)
     launch_bwd<128, 0>(a, dbias, clear, s);

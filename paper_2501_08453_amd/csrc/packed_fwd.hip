@@ -636,7 +636,7 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(PackedArgs a) {
 
 template <int D, int RMAX>
 void launch(PackedArgs a, hipStream_t s) {
-  const int clear = a.clear ? 32 : 0, heads = a.H / a.pack;
+  const int clear = a.clear ? kClearGroups : 0, heads = a.H / a.pack;
   set_blocks(a, a.pack > 1 ? 1 : a.max_q, a.Tq);  // heads packed into a block: one block a slot
   if (a.few) {
     hipLaunchKernelGGL((packed_few_kernel<D, RMAX>), dim3(heads * a.S * a.chunks + clear), dim3(64 * kFewWaves), 0, s, a);

@@ -152,3 +152,73 @@ def test_relative_buckets():
     assert b[65:] == [8 + x for x in behind[1:]]
     one = vc.relative_buckets(8, 64, bidirectional=False, device="cpu").tolist()
     assert one[64::-1] == behind and one[65:] == [0] * 64
+
+
+def test_launches_of_2_32_threads_and_more_are_refused(lib):
+    """Workgroups have 256 threads, 32 of them clear the rows outside the slots: a grid of 2^24 - 1 - 32 others is the largest."""
+    most = (2 ** 32 - 1) // 256 - 32
+
+    def one(S, H, Hkv, q=1, k=1, **kw):  # S slots of q queries and k keys
+        d = vc.make_packed_desc(S, H, Hkv, 64, S * q, S * k, q, k)
+        for n, x in kw.items():
+            setattr(d, n, x)
+        return d
+
+    def sizes(d):
+        return vc.vc_packedattn_fwd_workspace_bytes(d), vc.vc_packedattn_bwd_workspace_bytes(d)
+
+    def refused(d, f):
+        w = dict(bias=P, buckets=P) if d.num_buckets else {}
+        return f(lib, d, **w) == -2
+
+    # single tokens of 17 heads each: sequences x heads workgroups, in both directions
+    assert all(sizes(one(most // 17, 17, 17))) and sizes(one(most // 17 + 1, 17, 17)) == (0, 0)
+    d = one(most // 17 + 1, 17, 17)
+    assert refused(d, fwd) and refused(d, bwd)
+    # the heads of a group share a workgroup forward, not in dQ's pass
+    d = one(1 << 20, 32, 8)
+    assert sizes(d)[0] > 0 and sizes(d)[1] == 0 and refused(d, bwd)
+    # two blocks of 128 rows a slot, of the queries or of the keys alone
+    d = one(1 << 17, 64, 64, q=200)
+    assert sizes(d) == (0, 0) and refused(d, fwd) and refused(d, bwd)
+    d = one(1 << 17, 64, 64, k=200)
+    assert sizes(d)[0] > 0 and sizes(d)[1] == 0 and refused(d, bwd)
+    # with a bias a key block has a workgroup per query head at least
+    d = one(1 << 19, 40, 1, num_buckets=4, max_distance=8)
+    assert sizes(d) == (0, 0) and refused(d, bwd)
+    d = one(1 << 18, 40, 1, num_buckets=4, max_distance=8)
+    assert all(sizes(d))
+    import torch
+    if not torch.cuda.is_available():
+        assert fwd(lib, one(1 << 20, 32, 8)) == -6 and fwd(lib, one(1 << 17, 64, 64, k=200)) == -6
+
+    n = vc.vc_layernorm_desc((2 ** 32 - 1) // 256, 8193, 0, 1, 1e-5, 0, 0)  # a workgroup a row
+    assert vc.vc_layernorm_bwd_workspace_bytes(n) > 0
+    n.rows += 1
+    assert vc.vc_layernorm_bwd_workspace_bytes(n) == 0
+    assert lib.vc_layernorm_fwd(ctypes.byref(n), P, P, P, P, P, P, None) == -2
+    n.cols = 8192
+    assert vc.vc_layernorm_bwd_workspace_bytes(n) > 0
+
+
+def test_chunks_keep_to_the_launch_limit():
+    """Whatever the sizes, chunks and grids stay below 2^32 threads: the forward's chunks, as its workspace gives them,
+    times its other workgroups, and the waves that join them."""
+    import random
+    rng = random.Random(7)
+    split = 0
+    for _ in range(4000):
+        S, Hkv, G = 1 << rng.randint(0, 20), 1 << rng.randint(0, 6), 1 << rng.randint(0, 3)
+        q = rng.choice([1, 1, 2, 4])
+        total_k = min(1 << 30, S * (1 << rng.randint(0, 9)) + (1 << rng.randint(0, 22)))
+        d = vc.make_packed_desc(S, Hkv * G, Hkv, 64, S * q, total_k, q, 1 << rng.randint(0, 22), causal=True)
+        n = vc.vc_packedattn_fwd_workspace_bytes(d)
+        if not n:
+            continue
+        chunks = 1 if n == 256 else n // (d.total_q * d.heads * (64 + 2) * 4)
+        heads = Hkv if q * G <= 32 else Hkv * G  # rows of a group's heads together
+        assert S * heads * chunks + 32 < 2 ** 24
+        if chunks > 1:
+            split += 1
+            assert S * q * d.heads * 64 < 2 ** 32
+    assert split > 100
