@@ -88,7 +88,7 @@ def relative_buckets(num_buckets, max_distance, bidirectional=True, device="cuda
     num_buckets, max_distance = int(num_buckets), int(max_distance)
     half = num_buckets // 2 if bidirectional else num_buckets
     exact = half // 2
-    if exact < 1 or half > MAX_BUCKETS or not exact < max_distance <= MAX_DISTANCE:
+    if exact < 1 or num_buckets > MAX_BUCKETS or not exact < max_distance <= MAX_DISTANCE:
         raise ValueError("relative_buckets: %d buckets over distances up to %d" % (num_buckets, max_distance))
     wide = half - exact
     side, k = [], 0

@@ -222,3 +222,16 @@ def test_chunks_keep_to_the_launch_limit():
             split += 1
             assert S * q * d.heads * 64 < 2 ** 32
     assert split > 100
+
+
+@pytest.mark.parametrize("both", [False, True], ids=["one-sided", "bidirectional"])
+def test_relative_buckets_up_to_the_largest_table(both):
+    """Tables that a call takes, and none beyond."""
+    b = vc.relative_buckets(1024 if both else 1022, 512, both, device="cpu")  # one-sided: fewer than 512 exact ones
+    assert len(b) == 1025 and int(b.min()) == 0 and int(b.max()) < 1024
+    d = vc.make_packed_desc(1, 1, 1, 64, 1, 1, 1, 1, num_buckets=1024, max_distance=512)
+    assert vc.vc_packedattn_fwd_workspace_bytes(d) > 0
+    d.num_buckets = 1026
+    assert vc.vc_packedattn_fwd_workspace_bytes(d) == 0
+    with pytest.raises(ValueError, match="relative_buckets"):
+        vc.relative_buckets(1026, 512, both, device="cpu")
