@@ -311,7 +311,7 @@ def _autograd_functions():
         def forward(ctx, q, k, v, bias, desc, cu_q, cu_k, len_q, len_k, buckets):
             o, lse = packed_fwd(q, k, v, desc, cu_q, cu_k, len_q, len_k, bias, buckets)
             ctx.save_for_backward(q, k, v, bias, o, lse, cu_q, cu_k, len_q, len_k, buckets)
-            ctx.desc = desc
+            ctx.desc = vc_packedattn_desc.from_buffer_copy(desc)  # the caller may change theirs before the backward
             return o
 
         @staticmethod

@@ -235,3 +235,27 @@ def test_relative_buckets_up_to_the_largest_table(both):
     assert vc.vc_packedattn_fwd_workspace_bytes(d) == 0
     with pytest.raises(ValueError, match="relative_buckets"):
         vc.relative_buckets(1026, 512, both, device="cpu")
+
+
+def test_backward_keeps_the_forwards_descriptor(monkeypatch):
+    """A descriptor changed after the forward (reused for the next batch) does not reach the backward."""
+    torch = pytest.importorskip("torch")
+    from paper_2501_08453_amd import tower
+    seen = []
+
+    def forward(q, k, v, desc, *rest):
+        return torch.zeros_like(q), torch.zeros(q.shape[1], q.shape[0])
+
+    def backward(q, k, v, o, lse, do, desc, *rest, want_dbias):
+        seen.append((desc.causal, desc.softmax_scale, desc.max_k))
+        return torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v), None
+
+    monkeypatch.setattr(tower, "packed_fwd", forward)
+    monkeypatch.setattr(tower, "packed_bwd", backward)
+    q = torch.zeros((8, 2, 64), dtype=torch.bfloat16, requires_grad=True)
+    cu = torch.tensor([0, 8], dtype=torch.int32)
+    d = vc.make_packed_desc(1, 2, 2, 64, 8, 8, 8, 8, causal=True, scale=0.5)
+    o = vc.packed_attention(q, q, q, d, cu, cu)
+    d.causal, d.softmax_scale, d.max_k = 0, 0.25, 4
+    o.sum().backward()
+    assert seen == [(1, 0.5, 8)]
