@@ -110,6 +110,15 @@ def _launch(device, f, *args):
         return f(*args)
 
 
+def _ws_bytes(ws, device):
+    """Bytes of a workspace given by the caller: contiguous, on the device of the call's tensors (the kernels write to it)."""
+    if ws.device != device:
+        raise ValueError("ws is on %s, the call's tensors on %s" % (ws.device, device))
+    if not ws.is_contiguous():
+        raise ValueError("ws must be contiguous")
+    return ws.numel() * ws.element_size()
+
+
 def _token_stride(name, t):
     """Elements between the rows of consecutive tokens of a [tokens, heads, D] tensor whose heads are contiguous; 0
     where the whole tensor is."""
@@ -197,7 +206,8 @@ def packed_fwd(q, k, v, desc, cu_q, cu_k, len_q=None, len_k=None, bias=None, buc
     d = _check_packed(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets, (("out", out),), (), lse)
     d.clear_outside = 1 if clear else 0
     ws = packed_fwd_workspace(d, q.device) if ws is None else ws
-    _launch(q.device, vc_packedattn_fwd, d, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets, out, lse, ws, ws.numel())
+    _launch(q.device, vc_packedattn_fwd, d, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets, out, lse, ws,
+            _ws_bytes(ws, q.device))
     return out, lse
 
 
@@ -219,7 +229,7 @@ def packed_bwd(q, k, v, o, lse, dout, desc, cu_q, cu_k, len_q=None, len_k=None, 
     dbias = torch.empty_like(bias) if bias is not None and want_dbias else None
     ws = packed_bwd_workspace(d, q.device) if ws is None else ws
     _launch(q.device, vc_packedattn_bwd, d, q, k, v, o, lse, dout, cu_q, cu_k, len_q, len_k, bias, buckets, dq, dk, dv, dbias,
-            ws, ws.numel())
+            ws, _ws_bytes(ws, q.device))
     return dq, dk, dv, dbias
 
 
@@ -289,7 +299,8 @@ def layer_norm_bwd(dout, x, weight, bias, mean, rstd, ws=None):
     if desc.rows:
         if ws is None and (dw is not None or db is not None):
             ws = _workspace(vc_layernorm_bwd_workspace_bytes(desc), x.device)
-        _launch(x.device, vc_layernorm_bwd, desc, dout, x, weight, mean, rstd, dx, dw, db, ws, 0 if ws is None else ws.numel())
+        _launch(x.device, vc_layernorm_bwd, desc, dout, x, weight, mean, rstd, dx, dw, db, ws,
+                0 if ws is None else _ws_bytes(ws, x.device))
     return dx, dw, db
 
 

@@ -259,3 +259,26 @@ def test_backward_keeps_the_forwards_descriptor(monkeypatch):
     d.causal, d.softmax_scale, d.max_k = 0, 0.25, 4
     o.sum().backward()
     assert seen == [(1, 0.5, 8)]
+
+
+def test_workspace_on_another_device_is_refused(monkeypatch):
+    """The kernels write to it: nothing is launched. (Device and layout of the other tensors are left out here.)"""
+    torch = pytest.importorskip("torch")
+    from paper_2501_08453_amd import tower
+    launched = []
+    monkeypatch.setattr(tower, "_check_all", lambda every: None)
+    monkeypatch.setattr(tower, "_launch", lambda device, f, *args: launched.append(args[-1]))
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)  # noqa: E731
+    q, lse, cu = bf(8, 2, 64), torch.zeros(2, 8), torch.zeros(2, dtype=torch.int32)
+    x, w, mean = bf(4, 16), torch.ones(16), torch.zeros(4)
+    d = vc.make_packed_desc(1, 2, 2, 64, 8, 8, 8, 8)
+    calls = (lambda ws: vc.packed_fwd(q, q, q, d, cu, cu, ws=ws), lambda ws: vc.packed_bwd(q, q, q, q, lse, q, d, cu, cu, ws=ws),
+             lambda ws: vc.layer_norm_bwd(x, x, w, w, mean, mean, ws=ws))
+    for call in calls:
+        with pytest.raises(ValueError, match="ws is on meta"):
+            call(torch.empty(1 << 20, dtype=torch.uint8, device="meta"))
+        with pytest.raises(ValueError, match="ws must be contiguous"):
+            call(torch.empty(1, dtype=torch.uint8).expand(1 << 20))
+        assert not launched
+        call(torch.empty(1 << 10, dtype=torch.float32))
+        assert launched.pop() == 1 << 12
