@@ -427,3 +427,19 @@ def test_one_output_given(given):
         rows, ref = (t.t(), want[n].t()) if n == "lse" else (t, want[n])
         assert torch.equal(rows[a:b], ref[a:b]), n
         assert all((r == 7).all() if n == given else torch.equal(r, f) for r, f in ((rows[:a], ref[:a]), (rows[b:], ref[b:]))), n
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [False, True], ids=["full", "causal"])
+@pytest.mark.parametrize("R", [129, 300, 512])
+def test_distances_of_the_wide_table(R, causal, D):
+    """More queries and keys than any distance with a bucket of its own, on both sides, in the kernels for distances past 128; a
+    block of queries behind a longer cache, and fewer distances than R."""
+    check(*make(42, [1200, 90, 40], [1200, 1500, 40], 2, 2, D, causal, 8, R))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("nb", [256, 257, 1024])
+def test_large_tables(nb, D):
+    """Tables whose values are loaded along with the bucket numbers (up to 256), and larger ones."""
+    check(*make(43, [600, 3], [600, 70], 2, 2, D, False, nb, 512))
