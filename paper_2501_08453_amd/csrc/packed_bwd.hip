@@ -165,12 +165,13 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedA
   // Rows of at most one tile of keys: D = sum_j P_ij dP_ij itself, by a walk over that tile beforehand. Taken
   // of the rounded O it is off by about 2^-9 |dO| |O|, which moves all dS of the row by its P; over many
   // keys that is lost among dS's own rounding, but with a few keys of unequal weight dS is much smaller than
-  // D, and dQ of texts of a few tokens was off by 0.5% (2^-8 by its own rounding).
+  // D, and dQ of texts of a few tokens was off by 0.5% (2^-8 by its own rounding). Over the sum of P, which is 1 but for the
+  // rounding of LSE: with a bias of 10,000s that reaches 2^-8 and would move D by as much.
   if (kt0 < kt1 && b0 < sr.nq && limit(min(b0 + 32, sr.nq) - 1) <= kBN) {  // the first wave's last query
     __syncthreads();
     if (wave_keys > 0 && wave_keys <= kBN) {
       const VC_LDS char* rp = (const VC_LDS char*)smem + Reads::row_base(perm_row(l32), hi);
-      float sum = 0.0f;
+      float sum = 0.0f, all = 0.0f;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
         f32x16 s = zero_f32x16(), dp = zero_f32x16();
@@ -185,10 +186,14 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedA
           const int key = 32 * kb + acc_row(r, hi);
           float x = s[r];
           if (BIAS) x += b[min(max(key - pos0 - l32, -a.R), a.R)];
-          sum += key < klim ? fast_exp2(fmaf(x, a.scale_log2, nlse2)) * dp[r] : 0.0f;
+          const float p = key < klim ? fast_exp2(fmaf(x, a.scale_log2, nlse2)) : 0.0f;
+          all += p;
+          sum = fmaf(p, dp[r], sum);
         }
       }
-      dd = klim == 0 ? 0.0f : -halves_sum(sum);
+      all = halves_sum(all);
+      sum = halves_sum(sum);
+      dd = all > 0.0f ? -sum / all : 0.0f;
     }
   }
   for (int kt = kt0; kt < kt1; ++kt) {

@@ -443,3 +443,30 @@ def test_distances_of_the_wide_table(R, causal, D):
 def test_large_tables(nb, D):
     """Tables whose values are loaded along with the bucket numbers (up to 256), and larger ones."""
     check(*make(43, [600, 3], [600, 70], 2, 2, D, False, nb, 512))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [False, True], ids=["full", "causal"])
+def test_bias_above_the_limit(causal, D):
+    """Entries above 65536, +inf among them, count as 65536. Scores exact (whole q . k, scale 1). LSE of about 65536 is held in fp32,
+    half a step of which is h = 2^-8: rounded itself, with its base and the sum's logarithm in log2 units (h ln 2 each), and
+    by the constants log2 e and ln 2 (h each); P in the backward has the error of LSE, that of LSE in log2 units (h ln 2),
+    and far tiles' that of the bias in log2 units (h ln 2): 3 + 4 ln 2 < 6 of h in all."""
+    import torch
+    x, d, desc = make(44, [70, 9], [70, 200], 2, 1, D, causal, 4, 12, scale=1.0)
+    for n in ("q", "k"):
+        x[n] = np.clip(np.round(x[n]), -1, 1)
+        d[n] = torch.from_numpy(x[n]).to(torch.bfloat16).cuda()
+    d["bias"][:, 1], d["bias"][0, 2], d["bias"][1, 2] = 70000.0, float("inf"), 65536.0
+    x["bias"] = d["bias"].double().cpu().numpy()
+    x["buckets"][12] = 0  # a causal first row sees no large one
+    d["buckets"] = torch.from_numpy(x["buckets"]).cuda()
+    out = run(d, desc)
+    eps = 6 * 2.0 ** -8
+    r, tol = bounds(x, eps)
+    assert (r["lse"] > 65000).any() and (not causal or (r["lse"] < 100).any())
+    assert np.abs(out["lse"].double().cpu().numpy() - r["lse"]).max() <= eps
+    for n in tol:
+        off = np.abs(bf16_values(out[n]) - r[n]) / tol[n]
+        log("   %-5s off / bound %.3f" % (n, off.max()))
+        assert off.max() <= 1, n
