@@ -406,7 +406,8 @@ vc_status vc_offload_wait(vc_offload* h, void* stream);
  * and LSE, O, dQ, dK, dV as above (dK, dV summed over the query heads of a group) and
  * dbias[h][u] = the sum of dS_ij over the pairs of bucket u. Probabilities and sums are
  * fp32; P and dS are rounded to bf16 for the products with V, K, Q and dO (the matrix cores'
- * operands). A query that sees no key
+ * operands). D = <dO, O> is taken of the rounded o for queries of more than 64 keys; its rounding is
+ * taken out of dK and dbias, not of dQ. A query that sees no key
  * (causal, and more queries than keys; or shut out by the bias) gets O = 0, LSE = -inf,
  * dQ = 0. An entry of the bias below -65536 (-inf, or a type's lowest value) shuts its
  * pairs out: probability exactly 0; one above 65536 counts as 65536.

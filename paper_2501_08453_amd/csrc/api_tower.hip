@@ -111,7 +111,8 @@ struct FwdPlan {
   bool few, fits;  // fits: the launches can be made
 };
 // The chunks of least estimated time, in tiles of 64 keys x 128 rows (about 1.8 us at head_dim 128, half
-// of that at 64, with two workgroups a compute unit): rounds over 512 places, each workgroup 3 tiles
+// of that at 64): rounds over 512 places, two workgroups a compute unit (at head_dim 64 the forward and dK/dV
+// hold three, which the model leaves out), each workgroup 3 tiles
 // more than its keys for its start and its partial results, and the merge, a launch of about 6 us and
 // the partials' way to memory and back. `blocks` count by their keys (equal_blocks); `uneven` ones (the
 // causal rule's, longest first) fill their last round. `cost`:

@@ -10,9 +10,9 @@
 //   of the group, so that dK and dV of the shared head are summed in registers; where that leaves
 //   too few workgroups, each takes a run of those tiles and fp32 partials are summed afterwards.
 //   With a bias it also sums dS over every distance, in LDS.
-// Both are bound by the matrix rate for long rows: 12,000 tokens causal, 16 heads, 2 key heads, D = 128: dQ 783 us,
-// 1,130 TFLOP/s of its 6 D a pair, dK/dV 1,135 us, 1,039 of 8 D (the first, plain walks, operands read where they
-// are used and the statistics from memory: 6.5 ms for forward and backward, now 2.4). Short ones wait for a few
+// Both are bound by the matrix rate for long rows: 12,000 tokens causal, 16 heads, 2 key heads, D = 128: dQ 773 us,
+// 1,145 TFLOP/s of its 6 D a pair, dK/dV 1,115 us, 1,058 of 8 D (the first, plain walks, operands read where they
+// are used and the statistics from memory: 6.5 ms for forward and backward, now 2.4 to 2.5). Short ones wait for a few
 // tiles one after the other: captions of 8 to 256 tokens, 16 heads, D = 64, bias, 23 and 30 us.
 // No atomics anywhere: results are bitwise reproducible.
 #include "packed.hpp"
@@ -163,10 +163,12 @@ __global__ __launch_bounds__(64 * kPackedWaves, 2) void packed_dq_kernel(PackedA
 
   wait_all_memory();  // the loads above too: no later wait stands among copies
   // Rows of at most one tile of keys: D = sum_j P_ij dP_ij itself, by a walk over that tile beforehand. Taken
-  // of the rounded O it is off by about 2^-9 |dO| |O|, which moves all dS of the row by its P; over many
-  // keys that is lost among dS's own rounding, but with a few keys of unequal weight dS is much smaller than
-  // D, and dQ of texts of a few tokens was off by 0.5% (2^-8 by its own rounding). Over the sum of P, which is 1 but for the
+  // of the rounded O it is off by about 2^-9 |dO| |O|, which moves all dS of the row by its P; with a few keys
+  // of unequal weight dS is much smaller than D, and dQ of texts of a few tokens was off by 0.5% (2^-8 by its own rounding). Over the sum of P, which is 1 but for the
   // rounding of LSE: with a bias of 10,000s that reaches 2^-8 and would move D by as much.
+  // Over more keys dQ keeps the rounding of O (the other pass and the bias gradient do not: the row's sum of dS, below):
+  // off by 0.24% of its 2-norm beside 0.23% without it at 300 keys and scale 1/8, by 0.7% in sharp rows (scale 2).
+  // To take it out of dQ too, sum_j P_ij k_j would have to be summed beside dQ: a third more products.
   if (kt0 < kt1 && b0 < sr.nq && limit(min(b0 + 32, sr.nq) - 1) <= kBN) {  // the first wave's last query
     __syncthreads();
     if (wave_keys > 0 && wave_keys <= kBN) {
@@ -761,7 +763,8 @@ __global__ __launch_bounds__(256) void packed_key_sum_kernel(PackedArgs a, int p
 // Bias gradient, one workgroup per head: the blocks' sums per distance added up in order, then
 // the distances of each bucket. In both steps the threads share the sums of one result by runs,
 // which are then joined in order (one thread per result, bounds looked up at each block: 28 us for
-// captions of 8 to 256 tokens at 16 heads, so 6).
+// captions of 8 to 256 tokens at 16 heads, so 6; 1,024 such captions 63, 4,096 251, as the workgroups stay
+// one per head: a twentieth of the backward).
 __global__ __launch_bounds__(1024) void packed_dbias_kernel(PackedArgs a, __bf16* dbias) {
   __shared__ float part[1024];
   __shared__ float sum[2 * kMaxBiasDistance + 1];

@@ -2,7 +2,8 @@
 // other, grouped heads, causal or not, with an optional bias per bucket of the distance.
 //
 // One workgroup of four waves owns 128 query rows of one (sequence, head), each wave 32 held in
-// registers; two workgroups share a compute unit. (Eight waves and 256 rows, as in the joint forward,
+// registers; two workgroups share a compute unit at D = 128 (213 to 219 registers), three at D = 64 (147 to 149,
+// 37 to 43 KB of LDS). (Eight waves and 256 rows, as in the joint forward,
 // are 1% faster at 8,192 tokens and up and up to twice as slow below: 509 -> 504 us there, 48 -> 90 us
 // at 2,048, both at 32 heads, D = 128.) Keys and values stream through LDS in tiles of 64. The wave computes S^T = K Q^T, so that a lane's accumulator column is one query, and
 // O^T += V^T P^T with P^T straight from the accumulator layout. Software pipeline: at step j the
@@ -11,8 +12,8 @@
 // of 32 probabilities against it exceeds 2^13 (see the joint forward). Probabilities are summed
 // unrounded, so that LSE holds to fp32; they are rounded to bf16 for the product with V, the
 // matrix cores' operand type. Under the causal rule each wave stops at its own last tile.
-// What bounds it: the matrix rate for long rows (12,000 tokens causal, 16 heads, 2 key heads, D = 128: 571 us,
-// 1,033 TFLOP/s; a call of 8,192 x 8,192 uncausal, 16 heads: 554 us, 992 TFLOP/s, and at D = 64, which has as many
+// What bounds it: the matrix rate for long rows (12,000 tokens causal, 16 heads, 2 key heads, D = 128: 561 us,
+// 1,051 TFLOP/s; a call of 8,192 x 8,192 uncausal, 16 heads: 554 us, 992 TFLOP/s, and at D = 64, which has as many
 // exponentials for half the products, 300 us, 916), and the waits of a few tiles one after the other for short
 // ones (captions of 8 to 256 tokens with the bias, 16 heads, D = 64: 17 us).
 #include "packed.hpp"

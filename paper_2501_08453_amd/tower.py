@@ -357,5 +357,6 @@ def packed_attention(q, k, v, desc, cu_q, cu_k, len_q=None, len_k=None, bias=Non
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
-    """Differentiable layer norm over the last dimension of x: gradients of x, weight and bias."""
+    """Differentiable layer norm over the last dimension of x: gradients of x, weight and bias. For a captured graph take
+    layer_norm_fwd and layer_norm_bwd (see packed_attention)."""
     return _autograd_functions()["norm"].apply(x, weight, bias, eps)
