@@ -12,7 +12,7 @@
 //   With a bias it also sums dS over every distance, in LDS.
 // Both are bound by the matrix rate for long rows: 12,000 tokens causal, 16 heads, 2 key heads, D = 128: dQ 773 us,
 // 1,145 TFLOP/s of its 6 D a pair, dK/dV 1,115 us, 1,058 of 8 D (the first, plain walks, operands read where they
-// are used and the statistics from memory: 6.5 ms for forward and backward, now 2.4 to 2.5). Short ones wait for a few
+// are used and the statistics from memory: 6.5 ms for forward and backward, now 2.3 to 2.5 by the clock). Short ones wait for a few
 // tiles one after the other: captions of 8 to 256 tokens, 16 heads, D = 64, bias, 23 and 30 us.
 // No atomics anywhere: results are bitwise reproducible.
 #include "packed.hpp"
