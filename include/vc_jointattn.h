@@ -445,7 +445,8 @@ typedef struct vc_packedattn_desc {
   float softmax_scale;    /* c; <= 0 selects 1/sqrt(D). 2^-60 .. 2^60, with a bias 2^-24 .. 2^24 */
   int32_t num_buckets;    /* 0: no bias; up to 1024                             */
   int32_t max_distance;   /* R, 0 .. 512                                        */
-  int32_t clear_outside;  /* 1: outputs' rows outside every slot are written too */
+  int32_t clear_outside;  /* 1: outputs' rows outside every slot are written too;
+                             the forward's 2: those of o alone, 3: of lse alone */
 } vc_packedattn_desc;
 
 /* Bytes of device workspace of the forward (fp32 partial results where several workgroups

@@ -33,7 +33,7 @@ vc_status check_packed(const vc_packedattn_desc* d) {
   if (d->sequences > (1 << 20) || d->heads > 4096) return VC_ERR_SHAPE;
   if (d->total_q < 1 || d->total_q > kMaxRows || d->total_k < 1 || d->total_k > kMaxRows) return VC_ERR_SHAPE;
   if (d->max_q < 1 || d->max_q > d->total_q || d->max_k < 1 || d->max_k > d->total_k) return VC_ERR_SHAPE;
-  if ((d->causal & ~1) || (d->clear_outside & ~1)) return VC_ERR_SHAPE;
+  if ((d->causal & ~1) || (d->clear_outside & ~3)) return VC_ERR_SHAPE;
   const int64_t D = d->head_dim;
   for (const int64_t s : {d->q_stride, d->k_stride, d->v_stride})
     if (s < 0 || s > kMaxStride || s % 8) return VC_ERR_SHAPE;
@@ -299,6 +299,7 @@ vc_status check_fwd(const vc_packedattn_desc* d, FwdPlan* p) {
 vc_status check_bwd(const vc_packedattn_desc* d, BwdPlan* p) {
   const vc_status st = check_packed(d);
   if (st != VC_OK) return st;
+  if (d->clear_outside > 1) return VC_ERR_SHAPE;
   *p = bwd_plan(d);
   return p->fits ? VC_OK : VC_ERR_SHAPE;
 }

@@ -27,7 +27,7 @@ struct PackedArgs {
   int S, H, Hkv, G;        // G = H / Hkv query heads per key head
   int Tq, Tk, max_q, max_k;
   unsigned q_tok, k_tok, v_tok;  // elements between the rows of consecutive tokens
-  int causal, clear;
+  int causal, clear;  // clear: rows outside every slot, 1 of all outputs (forward: 2 of o, 3 of lse alone)
   float scale, scale_log2;  // softmax scale; times log2(e)
   int nblk, blocks;         // row blocks of the longest slot; of all slots in a grid
   bool compact;             // blocks numbered through (see packed_item)

@@ -70,7 +70,7 @@ __device__ __forceinline__ void wait_loads() {
 // Waits for this wave's LDS operations.
 __device__ __forceinline__ void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// O = 0 and LSE = -inf for the rows outside every slot (the last workgroups of a grid).
+// O = 0 and LSE = -inf, or one of them, for the rows outside every slot (the last workgroups of a grid).
 template <int D>
 __device__ __forceinline__ void clear_o(const PackedArgs& a, int wg, int wgs, int tid, int threads) {
   const int head = min(max(a.cu_q[0], 0), a.Tq), end = min(max(a.cu_q[a.S], head), a.Tq);
@@ -78,8 +78,8 @@ __device__ __forceinline__ void clear_o(const PackedArgs& a, int wg, int wgs, in
   for (int64_t i = (int64_t)wg * threads + tid; i < n; i += (int64_t)wgs * threads) {
     const int64_t rh = i / (D / 8);
     const int r0 = (int)(rh / a.H), h = (int)(rh % a.H), r = r0 < head ? r0 : r0 - head + end;
-    *(bf16x8*)(a.o + ((size_t)r * a.H + h) * D + i % (D / 8) * 8) = zero_bf16x8();
-    if (i % (D / 8) == 0) a.lse[(size_t)h * a.Tq + r] = -INFINITY;
+    if (a.clear != 3) *(bf16x8*)(a.o + ((size_t)r * a.H + h) * D + i % (D / 8) * 8) = zero_bf16x8();
+    if (a.clear != 2 && i % (D / 8) == 0) a.lse[(size_t)h * a.Tq + r] = -INFINITY;
   }
 }
 

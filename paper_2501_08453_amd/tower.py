@@ -7,7 +7,6 @@ every step of the computation runs in the library's HIP kernels (include/vc_join
 from __future__ import annotations
 
 import ctypes
-import math
 
 from paper_2501_08453_amd import (_call, _check_placed, _check_shape, _lib, _ptr, _stream, _workspace,
                                   vc_layernorm_desc, vc_packedattn_desc)
@@ -195,16 +194,13 @@ def packed_fwd(q, k, v, desc, cu_q, cu_k, len_q=None, len_k=None, bias=None, buc
     [cu_q[s], cu_q[s+1]) and [cu_k[s], cu_k[s+1]) or, of these, the first len_q[s] and len_k[s]. Rows outside every
     slot are 0 (lse: -inf) in each tensor made here, and left as they were in `out` or `lse` where that is given."""
     import torch
-    clear = out is None and lse is None  # by the library: both; where one is given, the other is filled beforehand
+    clear = (1 if lse is None else 2) if out is None else 3 if lse is None else 0  # both, out, lse, none
     if out is None:
-        new = torch.empty if clear else torch.zeros
-        out = new((desc.total_q, desc.heads, desc.head_dim), dtype=torch.bfloat16, device=q.device)
+        out = torch.empty((desc.total_q, desc.heads, desc.head_dim), dtype=torch.bfloat16, device=q.device)
     if lse is None:
-        shape = (desc.heads, desc.total_q)
-        lse = (torch.empty(shape, dtype=torch.float32, device=q.device) if clear
-               else torch.full(shape, -math.inf, dtype=torch.float32, device=q.device))
+        lse = torch.empty((desc.heads, desc.total_q), dtype=torch.float32, device=q.device)
     d = _check_packed(desc, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets, (("out", out),), (), lse)
-    d.clear_outside = 1 if clear else 0
+    d.clear_outside = clear
     ws = packed_fwd_workspace(d, q.device) if ws is None else ws
     _launch(q.device, vc_packedattn_fwd, d, q, k, v, cu_q, cu_k, len_q, len_k, bias, buckets, out, lse, ws,
             _ws_bytes(ws, q.device))

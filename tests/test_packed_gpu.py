@@ -470,3 +470,22 @@ def test_bias_above_the_limit(causal, D):
         off = np.abs(bf16_values(out[n]) - r[n]) / tol[n]
         log("   %-5s off / bound %.3f" % (n, off.max()))
         assert off.max() <= 1, n
+
+
+@pytest.mark.parametrize("given", ["out", "lse"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_one_output_given_to_a_single_token_step(given, D):
+    """The same in the few-row kernel, with keys shared by several workgroups."""
+    import torch
+    vc = _vc()
+    x, d, desc = make(45, [1, 0, 2], [5000, 4, 900], 8, 2, D, True, outside=(3, 40))
+    want = dict(zip(("out", "lse"), vc.packed_fwd(d["q"], d["k"], d["v"], desc, d["cu_q"], d["cu_k"], **_kw(d))))
+    kept = torch.full_like(want[given], 7.0)
+    got = dict(zip(("out", "lse"), vc.packed_fwd(d["q"], d["k"], d["v"], desc, d["cu_q"], d["cu_k"], **{given: kept}, **_kw(d))))
+    a, b = int(x["cu_q"][0]), int(x["cu_q"][-1])
+    for n, t in got.items():
+        ref = want[n].clone()
+        if n == given:
+            (ref.t() if n == "lse" else ref)[:a] = 7
+            (ref.t() if n == "lse" else ref)[b:] = 7
+        assert torch.equal(t, ref), n

@@ -282,3 +282,12 @@ def test_workspace_on_another_device_is_refused(monkeypatch):
         assert not launched
         call(torch.empty(1 << 10, dtype=torch.float32))
         assert launched.pop() == 1 << 12
+
+
+def test_clearing_one_output_is_the_forwards(lib):
+    """clear_outside 2 and 3 name the forward's outputs."""
+    for c, f, b in ((0, True, True), (1, True, True), (2, True, False), (3, True, False), (4, False, False)):
+        d = desc(clear_outside=c)
+        assert (vc.vc_packedattn_fwd_workspace_bytes(d) > 0) == f and (vc.vc_packedattn_bwd_workspace_bytes(d) > 0) == b
+        assert b or bwd(lib, d) == -2
+        assert f or fwd(lib, d) == -2
