@@ -31,7 +31,7 @@
  * a joint permutation of keys and values), so the paper's interleaving of text
  * and visual embeddings is an ordering choice the caller may make freely.
  *
- * Conventions for every entry point (the text tower's, at the end, have layouts of their own)
+ * Conventions for every entry point (those of the text tower and around a block's attention, at the end, have layouts of their own)
  *  - Tensors q, k, v, o, dout, dq, dk, dv: bf16, contiguous [B, N, H, D]
  *    (head_dim fastest), device memory, 16-byte aligned.
  *  - lse: fp32 [B, H, N], device memory, 16-byte aligned.
@@ -62,7 +62,7 @@ extern "C" {
 /* Raised with every change of a signature, a struct, the meaning of an argument or a
  * documented result; the Python binding refuses a library that reports another
  * version. */
-#define VC_JOINTATTN_ABI_VERSION 13
+#define VC_JOINTATTN_ABI_VERSION 14
 
 typedef enum vc_status {
   VC_OK = 0,
@@ -515,6 +515,137 @@ vc_status vc_layernorm_bwd(const vc_layernorm_desc* desc,
                            const void* dout, const void* x, const void* weight,
                            const float* mean, const float* rstd,
                            void* dx, void* dweight, void* dbias,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Gated residual with the norms before and after a block: what stands between one block's
+ * attention and the next one's. With the vectors gate, scale and shift of row r's sample (a clip, a caption; a block's
+ * modulation, or learned and then shared by all samples), the stream x takes in the block's output a,
+ *
+ *   h = c x + gate P(a),      P(a) = a, or a normed and multiplied by post_weight,
+ *   y = N(h) e + shift,       e = scale or, with `plus_one`, 1 + scale,
+ *
+ * where a layer norm is (t - mean t) r, r = 1 / sqrt(mean of (t - mean t)^2 + eps), and an RMS norm t r,
+ * r = 1 / sqrt(mean of t^2 + eps). h is rounded to the stream's type first; the norm takes the rounded h.
+ * Backward, from the gradients dh (of h, as the blocks behind leave it) and dy, with xh = N(h) and xa = P(a)
+ * before post_weight: H = dh + (dy e through N), dx = c H, da = (H gate post_weight through P, or H gate), and
+ *   dgate = post_weight sum H xa, dscale = sum dy xh, dshift = sum dy (over the sample's rows, or all of them where the
+ *   vector is shared), dpost_weight = sum over samples of gate sum H xa.
+ * Statistics and sums in fp32, in a fixed order (no atomics).
+ *  - Samples: `rows` in `samples` equal slots; or, with `packed`, rows [cu[s], cu[s+1]) of device int32 cu [samples + 1],
+ *    not decreasing. The first lens[s] rows of a slot take part (device int32 [samples] or NULL: all of them). Both arrays
+ *    are read on the device only; nothing outside the tensors is read or written whatever they hold.
+ *  - Rows of a slot behind its length get h = y = 0, dx = da = 0; what the inputs hold there has no effect. Rows
+ *    outside every slot are left as they were, or with `clear_outside` written as those.
+ *  - gate NULL: 1; scale NULL: e = 1; shift NULL: 0; post_weight NULL: 1. a NULL (a norm alone; c = 1, no
+ *    gate and no post_norm): h = x, written unless h is NULL. norm VC_NORM_NONE (the residual alone): no y.
+ *  - With `checkpoint` the forward writes what its backward needs of h and a in 8 bits beside them (see
+ *    vc_checkpoint_pack: h8, a8 int8 [rows, cols], scales fp32 [rows, ceil(cols / 128)]), and the backward takes these in
+ *    place of h and a.
+ *  - x, dh: x_type, a, dy: y_type, rows x_stride, a_stride, dh_stride, dy_stride apart; h, dx of x_type and y, da of
+ *    y_type: contiguous. VC_BF16 or VC_FP32 each, but not VC_BF16 with a y_type of VC_FP32. Vectors of param_type, those of consecutive samples
+ *    gate_stride, ... elements apart (0: cols; VC_SHARED: one for all samples); their gradients contiguous
+ *    [samples, cols], or [cols] where shared; with one sample either. mean, rstd, post_mean, post_rstd: fp32 [rows], means unused by RMS norms.
+ *    Pointers aligned to their element.
+ * ------------------------------------------------------------------------- */
+#define VC_NORM_NONE 0
+#define VC_NORM_LAYER 1
+#define VC_NORM_RMS 2
+#define VC_SHARED (-1)
+
+typedef struct vc_residualnorm_desc {
+  int64_t rows;           /* 1 .. 2^30                                          */
+  int32_t cols;           /* 1 .. 8192                                          */
+  int32_t samples;        /* >= 1; ceil(cols / 64) * samples below 2^22; divides rows unless packed */
+  int32_t x_type;         /* VC_BF16 or VC_FP32: x, h, dh, dx                   */
+  int32_t y_type;         /* a, y, dy, da                                       */
+  int32_t param_type;     /* gate, scale, shift, post_weight, their gradients   */
+  int32_t norm;           /* N: VC_NORM_*                                       */
+  int32_t post_norm;      /* P: VC_NORM_*                                       */
+  int32_t packed;         /* 1: slots by cu                                     */
+  int32_t plus_one;       /* 1: e = 1 + scale                                   */
+  int32_t checkpoint;     /* 1: h and a for the backward in 8 bits              */
+  int32_t clear_outside;  /* 1: outputs' rows outside every slot are written too */
+  float residual_scale;   /* c                                                  */
+  float eps;              /* >= 0, of both norms                                */
+  int64_t x_stride;       /* elements between rows; 0: cols                     */
+  int64_t a_stride;
+  int64_t dh_stride;
+  int64_t dy_stride;
+  int64_t gate_stride;    /* elements between samples; 0: cols; or VC_SHARED    */
+  int64_t scale_stride;
+  int64_t shift_stride;
+} vc_residualnorm_desc;
+
+vc_status vc_residualnorm_fwd(const vc_residualnorm_desc* desc,
+                              const void* x, const void* a,
+                              const void* gate, const void* scale, const void* shift, const void* post_weight,
+                              const int32_t* cu, const int32_t* lens,
+                              void* h, void* y, float* mean, float* rstd, float* post_mean, float* post_rstd,
+                              void* h8, float* h8_scales, void* a8, float* a8_scales, void* stream);
+
+/* Bytes of device workspace of the backward (runs' and samples' column sums); 0 for an invalid descriptor. Host only. */
+size_t vc_residualnorm_bwd_workspace_bytes(const vc_residualnorm_desc* desc);
+
+/* h and a: as the forward had them (h written by it, a contiguous or a_stride apart), or its h8 and a8 with their scales.
+ * dh or dy may be NULL (0), every output too (not wanted); without the vectors' gradients the workspace may be NULL. */
+vc_status vc_residualnorm_bwd(const vc_residualnorm_desc* desc,
+                              const void* dh, const void* dy, const void* h, const void* a,
+                              const float* h8_scales, const float* a8_scales,
+                              const void* gate, const void* scale, const void* post_weight,
+                              const int32_t* cu, const int32_t* lens,
+                              const float* mean, const float* rstd, const float* post_mean, const float* post_rstd,
+                              void* dx, void* da, void* dgate, void* dscale, void* dshift, void* dpost_weight,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Activation checkpoints in 8 bits (Sec. V-B trades activation memory against time; this keeps
+ * an activation at half of its 16 bits). Each block of 128 columns of a row (the last one may be shorter), with
+ * m = max(the largest |x| of the block, 2^-100):
+ *   scale = m / 127, q = x * (127 / m) rounded to the nearest whole number (ties to even), -127 .. 127, x' = q * scale,
+ * in fp32: off by at most half a step, m / 254, and that rounding. A block that holds an infinity or a NaN has a scale of NaN, and
+ * unpacks to NaN. q: int8 [rows, cols], scales: fp32 [rows, ceil(cols / 128)], both contiguous.
+ * ------------------------------------------------------------------------- */
+typedef struct vc_checkpoint_desc {
+  int64_t rows;           /* 1 .. 2^32                                          */
+  int32_t cols;           /* 1 .. 2^24                                          */
+  int32_t type;           /* VC_BF16 or VC_FP32: of x, or of the unpacked y     */
+  int64_t stride;         /* elements between the rows of x; 0: cols. y is contiguous */
+} vc_checkpoint_desc;
+
+vc_status vc_checkpoint_pack(const vc_checkpoint_desc* desc, const void* x, void* q, float* scales, void* stream);
+vc_status vc_checkpoint_unpack(const vc_checkpoint_desc* desc, const void* q, const float* scales, void* y, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Embedding of tokens, the first step of a text tower: out_t = scale * table[ids_t], and its gradient
+ * dtable_v = scale * (sum of dout_t over the tokens t with ids_t = v), by tokens sorted by their ids:
+ * fp32 sums of shares of the sorted list, each in the order of t, in a division that follows from tokens and vocab alone;
+ * no atomics. A token of the padding id, or of an id outside 0 .. vocab - 1, gets out = 0 and gives no gradient.
+ *  - table, dtable: [vocab, cols] of table_type; out, dout: [tokens, cols] of out_type. The rows of table (forward) and dout
+ *    (backward) row_stride apart, out and dtable contiguous. Pointers aligned to their element.
+ *  - dtable is written whole, rows of ids that no token has as 0; with `accumulate` the sums are added to what is there (one
+ *    rounding to its type), and other rows are not touched.
+ * ------------------------------------------------------------------------- */
+typedef struct vc_embedding_desc {
+  int64_t tokens;         /* 1 .. 2^30, of a backward 1 .. 2^24                 */
+  int64_t vocab;          /* 1 .. 2^27                                          */
+  int64_t padding_id;     /* negative: none                                     */
+  int64_t row_stride;     /* elements between rows; 0: cols                     */
+  int32_t cols;           /* 1 .. 8192                                          */
+  int32_t ids64;          /* 0: int32 ids, 1: int64                             */
+  int32_t table_type;     /* VC_BF16 or VC_FP32                                 */
+  int32_t out_type;
+  float scale;
+  int32_t accumulate;     /* backward: 0 or 1                                   */
+} vc_embedding_desc;
+
+vc_status vc_embedding_fwd(const vc_embedding_desc* desc, const void* ids, const void* table, void* out, void* stream);
+
+/* Bytes of device workspace of the backward (sorted tokens, sums of ids that fill several shares); 0 for an invalid
+ * descriptor. Host only. */
+size_t vc_embedding_bwd_workspace_bytes(const vc_embedding_desc* desc);
+
+vc_status vc_embedding_bwd(const vc_embedding_desc* desc, const void* ids, const void* dout, void* dtable,
                            void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus

@@ -18,7 +18,7 @@ HEADER = os.path.join(os.path.dirname(PKG_DIR), "include", "vc_jointattn.h")
 # The ABI the signatures below describe (VC_JOINTATTN_ABI_VERSION of include/vc_jointattn.h);
 # a library reporting another version is refused, so that no call can reach an entry point
 # whose arguments differ from what this binding passes.
-ABI_VERSION = 13
+ABI_VERSION = 14
 # Bytes of the no-allocation forward's fixed scratch array (VC_JOINTATTN_NOALLOC_SCRATCH_BYTES).
 NOALLOC_SCRATCH_BYTES = 256 << 20
 
@@ -84,11 +84,64 @@ class vc_layernorm_desc(ctypes.Structure):
     ]
 
 
+class vc_residualnorm_desc(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int32),
+        ("samples", ctypes.c_int32),
+        ("x_type", ctypes.c_int32),
+        ("y_type", ctypes.c_int32),
+        ("param_type", ctypes.c_int32),
+        ("norm", ctypes.c_int32),
+        ("post_norm", ctypes.c_int32),
+        ("packed", ctypes.c_int32),
+        ("plus_one", ctypes.c_int32),
+        ("checkpoint", ctypes.c_int32),
+        ("clear_outside", ctypes.c_int32),
+        ("residual_scale", ctypes.c_float),
+        ("eps", ctypes.c_float),
+        ("x_stride", ctypes.c_int64),
+        ("a_stride", ctypes.c_int64),
+        ("dh_stride", ctypes.c_int64),
+        ("dy_stride", ctypes.c_int64),
+        ("gate_stride", ctypes.c_int64),
+        ("scale_stride", ctypes.c_int64),
+        ("shift_stride", ctypes.c_int64),
+    ]
+
+
+class vc_checkpoint_desc(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int32),
+        ("type", ctypes.c_int32),
+        ("stride", ctypes.c_int64),
+    ]
+
+
+class vc_embedding_desc(ctypes.Structure):
+    _fields_ = [
+        ("tokens", ctypes.c_int64),
+        ("vocab", ctypes.c_int64),
+        ("padding_id", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64),
+        ("cols", ctypes.c_int32),
+        ("ids64", ctypes.c_int32),
+        ("table_type", ctypes.c_int32),
+        ("out_type", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("accumulate", ctypes.c_int32),
+    ]
+
+
 _LIB = None
 _P = ctypes.c_void_p
 _DP = ctypes.POINTER(vc_jointattn_desc)
 _PP = ctypes.POINTER(vc_packedattn_desc)
 _NP = ctypes.POINTER(vc_layernorm_desc)
+_RP = ctypes.POINTER(vc_residualnorm_desc)
+_CP = ctypes.POINTER(vc_checkpoint_desc)
+_EP = ctypes.POINTER(vc_embedding_desc)
 _SIGS = {
     "vc_jointattn_abi_version": (ctypes.c_int, []),
     "vc_status_string": (ctypes.c_char_p, [ctypes.c_int]),
@@ -123,6 +176,14 @@ _SIGS = {
     "vc_layernorm_fwd": (ctypes.c_int, [_NP] + [_P] * 7),
     "vc_layernorm_bwd_workspace_bytes": (ctypes.c_size_t, [_NP]),
     "vc_layernorm_bwd": (ctypes.c_int, [_NP] + [_P] * 9 + [ctypes.c_size_t, _P]),
+    "vc_residualnorm_fwd": (ctypes.c_int, [_RP] + [_P] * 19),
+    "vc_residualnorm_bwd_workspace_bytes": (ctypes.c_size_t, [_RP]),
+    "vc_residualnorm_bwd": (ctypes.c_int, [_RP] + [_P] * 22 + [ctypes.c_size_t, _P]),
+    "vc_checkpoint_pack": (ctypes.c_int, [_CP] + [_P] * 4),
+    "vc_checkpoint_unpack": (ctypes.c_int, [_CP] + [_P] * 4),
+    "vc_embedding_fwd": (ctypes.c_int, [_EP] + [_P] * 4),
+    "vc_embedding_bwd_workspace_bytes": (ctypes.c_size_t, [_EP]),
+    "vc_embedding_bwd": (ctypes.c_int, [_EP] + [_P] * 4 + [ctypes.c_size_t, _P]),
 }
 
 
@@ -613,3 +674,9 @@ from .tower import (layer_norm, layer_norm_bwd, layer_norm_fwd, make_packed_desc
                     packed_bwd, packed_bwd_workspace, packed_fwd, packed_fwd_workspace, relative_buckets,
                     vc_layernorm_bwd, vc_layernorm_bwd_workspace_bytes, vc_layernorm_fwd, vc_packedattn_bwd,
                     vc_packedattn_bwd_workspace_bytes, vc_packedattn_fwd, vc_packedattn_fwd_workspace_bytes)
+
+# The operators around a block's attention (gated residual norms, 8-bit checkpoints, embedding).
+from .blocks import (Packed8, ResidualSaved, checkpoint_pack, checkpoint_unpack, embedding, embedding_bwd,  # noqa: E402,F401
+                     embedding_fwd, make_residual_desc, residual_norm, residual_norm_bwd, residual_norm_fwd, saved_in_8bit,
+                     vc_checkpoint_pack, vc_checkpoint_unpack, vc_embedding_bwd, vc_embedding_bwd_workspace_bytes,
+                     vc_embedding_fwd, vc_residualnorm_bwd, vc_residualnorm_bwd_workspace_bytes, vc_residualnorm_fwd)

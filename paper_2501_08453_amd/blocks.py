@@ -1,0 +1,446 @@
+"""The operators around a block's attention: the gated residual with the norms before and after a block, activation
+checkpoints in 8 bits, and the embedding of tokens.
+
+As everywhere in this package, the tensor-level helpers check and marshal arguments and allocate outputs;
+every step of the computation runs in the library's HIP kernels (include/vc_jointattn.h).
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import NamedTuple
+
+from paper_2501_08453_amd import (_call, _lib, _ptr, _stream, _workspace, vc_checkpoint_desc, vc_embedding_desc,
+                                  vc_residualnorm_desc)
+from paper_2501_08453_amd.tower import _check_all, _launch, _row_stride, _ws_bytes
+
+NORMS = {None: 0, "layer": 1, "rms": 2}  # VC_NORM_*
+SHARED = -1                              # VC_SHARED
+BLOCK = 128                              # columns of a row that share a checkpoint's scale
+
+
+# --------------------------------------------------------------------------
+# Raw entry points with the C names (pointers are ints or torch tensors).
+# --------------------------------------------------------------------------
+
+def vc_residualnorm_fwd(desc, x, a, gate, scale, shift, post_weight, cu, lens, h, y, mean, rstd, post_mean, post_rstd,
+                        h8, h8_scales, a8, a8_scales, stream=None):
+    _call("vc_residualnorm_fwd", ctypes.byref(desc), _ptr(x), _ptr(a), _ptr(gate), _ptr(scale), _ptr(shift),
+          _ptr(post_weight), _ptr(cu), _ptr(lens), _ptr(h), _ptr(y), _ptr(mean), _ptr(rstd), _ptr(post_mean),
+          _ptr(post_rstd), _ptr(h8), _ptr(h8_scales), _ptr(a8), _ptr(a8_scales), _stream(stream))
+
+
+def vc_residualnorm_bwd_workspace_bytes(desc) -> int:
+    return _lib().vc_residualnorm_bwd_workspace_bytes(ctypes.byref(desc))
+
+
+def vc_residualnorm_bwd(desc, dh, dy, h, a, h8_scales, a8_scales, gate, scale, post_weight, cu, lens, mean, rstd,
+                        post_mean, post_rstd, dx, da, dgate, dscale, dshift, dpost_weight, workspace, workspace_bytes,
+                        stream=None):
+    _call("vc_residualnorm_bwd", ctypes.byref(desc), _ptr(dh), _ptr(dy), _ptr(h), _ptr(a), _ptr(h8_scales),
+          _ptr(a8_scales), _ptr(gate), _ptr(scale), _ptr(post_weight), _ptr(cu), _ptr(lens), _ptr(mean), _ptr(rstd),
+          _ptr(post_mean), _ptr(post_rstd), _ptr(dx), _ptr(da), _ptr(dgate), _ptr(dscale), _ptr(dshift),
+          _ptr(dpost_weight), _ptr(workspace), int(workspace_bytes), _stream(stream))
+
+
+def vc_checkpoint_pack(desc, x, q, scales, stream=None):
+    _call("vc_checkpoint_pack", ctypes.byref(desc), _ptr(x), _ptr(q), _ptr(scales), _stream(stream))
+
+
+def vc_checkpoint_unpack(desc, q, scales, y, stream=None):
+    _call("vc_checkpoint_unpack", ctypes.byref(desc), _ptr(q), _ptr(scales), _ptr(y), _stream(stream))
+
+
+def vc_embedding_fwd(desc, ids, table, out, stream=None):
+    _call("vc_embedding_fwd", ctypes.byref(desc), _ptr(ids), _ptr(table), _ptr(out), _stream(stream))
+
+
+def vc_embedding_bwd_workspace_bytes(desc) -> int:
+    return _lib().vc_embedding_bwd_workspace_bytes(ctypes.byref(desc))
+
+
+def vc_embedding_bwd(desc, ids, dout, dtable, workspace, workspace_bytes, stream=None):
+    _call("vc_embedding_bwd", ctypes.byref(desc), _ptr(ids), _ptr(dout), _ptr(dtable), _ptr(workspace),
+          int(workspace_bytes), _stream(stream))
+
+
+# --------------------------------------------------------------------------
+# Gated residual with the norms before and after a block
+# --------------------------------------------------------------------------
+
+def make_residual_desc(rows, cols, samples=1, norm="layer", post_norm=None, residual_scale=1.0, eps=1e-5, plus_one=True,
+                       checkpoint=False):
+    """Descriptor of a gated residual over rows x cols of `samples` samples: h = residual_scale * x + gate * P(a),
+    y = N(h) * (1 + scale) + shift (plus_one False: N(h) * scale + shift). norm (N) and post_norm (P): "layer", "rms" or None.
+    checkpoint: what the backward needs of h and a is kept in 8 bits (see checkpoint_pack)."""
+    for k in (norm, post_norm):
+        if k not in NORMS:
+            raise ValueError('a norm is "layer", "rms" or None, got %r' % (k,))
+    return vc_residualnorm_desc(int(rows), int(cols), int(samples), 0, 0, 0, NORMS[norm], NORMS[post_norm], 0,
+                                1 if plus_one else 0, 1 if checkpoint else 0, 1, float(residual_scale), float(eps))
+
+
+class Packed8(NamedTuple):
+    """A tensor in 8 bits: q int8 of its shape, scales fp32 [..., ceil(columns / 128)], and the type it had."""
+    q: object
+    scales: object
+    dtype: object
+
+
+class ResidualSaved(NamedTuple):
+    """What a residual_norm_bwd takes of its forward. h and a: tensors, or with a checkpoint Packed8. The statistics of rows
+    that take no part are not defined."""
+    desc: object
+    h: object
+    a: object
+    gate: object
+    scale: object
+    shift: object
+    post_weight: object
+    cu: object
+    lens: object
+    mean: object
+    rstd: object
+    post_mean: object
+    post_rstd: object
+    y_dtype: object
+
+
+def _type(name, t):
+    import torch
+    if t.dtype is torch.bfloat16:
+        return 0
+    if t.dtype is torch.float32:
+        return 1
+    raise ValueError("%s must be torch.bfloat16 or torch.float32, got %s" % (name, t.dtype))
+
+
+def _vector(name, p, d, every, dtype):
+    """Appends a parameter to the checks; its stride between samples."""
+    cols, S = d.cols, d.samples
+    if p.dim() == 1:
+        every.append((name, p, (cols,), dtype, False))
+        return SHARED
+    every.append((name, p, (S, cols), dtype, True))
+    if p.is_contiguous() or S == 1 and p.stride(-1) == 1:
+        return 0
+    if p.dim() != 2 or p.stride(1) != 1 or p.stride(0) < cols:
+        raise ValueError("%s must be [columns], or [samples, columns] with contiguous rows" % name)
+    return p.stride(0)
+
+
+def _residual_desc(desc, x, a, gate, scale, shift, post_weight, cu, lens, y_dtype, dh=None, dy=None):
+    """A copy of the descriptor with the types and strides of the tensors of one call, checked."""
+    import torch
+    d = vc_residualnorm_desc.from_buffer_copy(desc)
+    shape = (d.rows, d.cols)
+    every = []
+    if x is not None:
+        d.x_type = _type("x", x)
+        every.append(("x", x, shape, x.dtype, True))
+        d.x_stride = _row_stride("x", x)
+    if a is not None:
+        d.y_type = _type("a", a)
+        every.append(("a", a, shape, a.dtype, True))
+        d.a_stride = _row_stride("a", a)
+    else:
+        d.y_type = 1 if y_dtype is torch.float32 else 0
+    first = next((p for p in (gate, scale, shift, post_weight) if p is not None), None)
+    if first is not None:
+        d.param_type = _type("gate, scale, shift and post_weight", first)
+        if gate is not None:
+            d.gate_stride = _vector("gate", gate, d, every, first.dtype)
+        if scale is not None:
+            d.scale_stride = _vector("scale", scale, d, every, first.dtype)
+        if shift is not None:
+            d.shift_stride = _vector("shift", shift, d, every, first.dtype)
+        if post_weight is not None:
+            every.append(("post_weight", post_weight, (d.cols,), first.dtype, False))
+    if cu is not None:
+        d.packed = 1
+        every.append(("cu", cu, (d.samples + 1,), torch.int32, False))
+    if lens is not None:
+        every.append(("lens", lens, (d.samples,), torch.int32, False))
+    if dh is not None:
+        every.append(("dh", dh, shape, torch.float32 if d.x_type else torch.bfloat16, True))
+        d.dh_stride = _row_stride("dh", dh)
+    if dy is not None:
+        every.append(("dy", dy, shape, torch.float32 if d.y_type else torch.bfloat16, True))
+        d.dy_stride = _row_stride("dy", dy)
+    _check_all(every)
+    return d
+
+
+def _kept(rows, cols, device, dtype):
+    import torch
+    return Packed8(torch.empty((rows, cols), dtype=torch.int8, device=device),
+                   torch.empty((rows, (cols + BLOCK - 1) // BLOCK), dtype=torch.float32, device=device), dtype)
+
+
+def residual_norm_fwd(x, a, desc, gate=None, scale=None, shift=None, post_weight=None, cu=None, lens=None, y_dtype=None):
+    """(h, y, saved): the residual stream x [rows, columns] with a block's output a taken in, and its norm for the next
+    block; `saved` is what residual_norm_bwd takes. a None: the norm alone (h is x). gate, scale, shift: [columns],
+    shared by all samples, or [samples, columns], of which consecutive samples may lie further apart, as in slices of one
+    projection. Rows are in equal slots, or with cu (int32 [samples + 1]) in those; the first lens[s] (int32 [samples]) of a
+    slot take part. All other rows of h and y are 0. x and a: bf16 or fp32 (a not fp32 with x bf16), rows may lie further apart; h has x's
+    type, y a's (without a: y_dtype, or x's)."""
+    import torch
+    if y_dtype is None:
+        y_dtype = x.dtype if a is None else a.dtype
+    elif a is not None and y_dtype is not a.dtype:
+        raise ValueError("y has a's type, %s" % a.dtype)
+    elif y_dtype is not torch.bfloat16 and y_dtype is not torch.float32:
+        raise ValueError("y_dtype must be torch.bfloat16 or torch.float32, got %s" % y_dtype)
+    d = _residual_desc(desc, x, a, gate, scale, shift, post_weight, cu, lens, y_dtype)
+    rows, cols, dev, f32 = d.rows, d.cols, x.device, torch.float32
+    h = x if a is None else torch.empty((rows, cols), dtype=x.dtype, device=dev)
+    y = mean = rstd = pmean = prstd = h8 = a8 = None
+    if d.norm:
+        y = torch.empty((rows, cols), dtype=y_dtype, device=dev)
+    if d.norm or d.post_norm:
+        mean, rstd, pmean, prstd = torch.empty((4, rows), dtype=f32, device=dev).unbind(0)
+    if d.checkpoint:
+        h8 = _kept(rows, cols, dev, x.dtype) if d.norm else None
+        a8 = None if a is None else _kept(rows, cols, dev, a.dtype)
+    _launch(dev, vc_residualnorm_fwd, d, x, a, gate, scale, shift, post_weight, cu, lens, None if a is None else h, y, mean, rstd,
+            pmean, prstd, h8 and h8.q, h8 and h8.scales, a8 and a8.q, a8 and a8.scales)
+    kept = (h8, a8) if d.checkpoint else (h if d.norm else None, a)
+    return h, y, ResidualSaved(d, *kept, gate, scale, shift, post_weight, cu, lens, mean, rstd, pmean, prstd, y_dtype)
+
+
+def residual_norm_bwd(dh, dy, saved, ws=None, want=(True,) * 6):
+    """(dx, da, dgate, dscale, dshift, dpost_weight) from the gradients of h and y (either may be None: 0) and what the
+    forward saved; None where there was no such input, or where `want` has it as not wanted. Vectors' gradients have their
+    vectors' shape. Rows that take no part are 0."""
+    import torch
+    s = saved
+    if s.desc.checkpoint:
+        h, a, hs, as_ = s.h and s.h.q, s.a and s.a.q, s.h and s.h.scales, s.a and s.a.scales
+    else:
+        h, a, hs, as_ = s.h, s.a, None, None
+    if dh is None and dy is None:
+        raise ValueError("dh and dy are both None")
+    d = vc_residualnorm_desc.from_buffer_copy(s.desc)
+    shape, every = (d.rows, d.cols), []
+    types = (torch.bfloat16, torch.float32)
+    first = dh if dh is not None else dy
+    if dh is not None:
+        every.append(("dh", dh, shape, types[d.x_type], True))
+        d.dh_stride = _row_stride("dh", dh)
+    if dy is not None:
+        if not d.norm:
+            raise ValueError("there is no y without a norm")
+        every.append(("dy", dy, shape, types[d.y_type], True))
+        d.dy_stride = _row_stride("dy", dy)
+    stat = s.rstd if s.rstd is not None else a
+    if stat is not None:
+        every.append(("saved", stat, stat.shape, stat.dtype, True))
+    _check_all(every)
+    if not d.norm and dh is None:
+        raise ValueError("there is no y without a norm")
+    dev = first.device
+    new = lambda like, t=None: torch.empty(like, dtype=t, device=dev)  # noqa: E731
+    dx = new(shape, types[d.x_type]) if want[0] else None
+    da = new(shape, types[d.y_type]) if a is not None and want[1] else None
+    dg, de, df, dw = (None if p is None or not w else new(p.shape, p.dtype)
+                      for p, w in zip((s.gate, s.scale, s.shift, s.post_weight), want[2:]))
+    if dx is None and da is None and dg is None and de is None and df is None and dw is None:
+        return (None,) * 6
+    if ws is None and not (dg is None and de is None and df is None and dw is None):
+        ws = _workspace(vc_residualnorm_bwd_workspace_bytes(d), dev)
+    _launch(dev, vc_residualnorm_bwd, d, dh, dy, h, a, hs, as_, s.gate, s.scale, s.post_weight, s.cu, s.lens, s.mean, s.rstd,
+            s.post_mean, s.post_rstd, dx, da, dg, de, df, dw, ws, 0 if ws is None else _ws_bytes(ws, dev))
+    return dx, da, dg, de, df, dw
+
+
+# --------------------------------------------------------------------------
+# Activation checkpoints in 8 bits
+# --------------------------------------------------------------------------
+
+def _rows_of(x):
+    """(rows, columns, stride) of x as rows of its last dimension."""
+    if x.dim() == 0 or x.numel() == 0:
+        return 0, x.shape[-1] if x.dim() else 1, 0
+    return x.numel() // x.shape[-1], x.shape[-1], _row_stride("x", x)
+
+
+def checkpoint_pack(x):
+    """x (bf16 or fp32; contiguous, or [rows, columns] with rows further apart) in 8 bits, a scale for each 128
+    columns: a Packed8 of 1 + 1/32 bytes an element. Off by at most half a step, the largest |x| of the 128 over 254; a block
+    that holds an infinity or a NaN unpacks to NaN."""
+    import torch
+    f32 = _type("x", x)
+    rows, cols, stride = _rows_of(x)
+    _check_all([("x", x, x.shape, x.dtype, True)])
+    kept = Packed8(torch.empty(x.shape, dtype=torch.int8, device=x.device),
+                   torch.empty(x.shape[:-1] + ((cols + BLOCK - 1) // BLOCK,), dtype=torch.float32, device=x.device), x.dtype)
+    if rows:
+        _launch(x.device, vc_checkpoint_pack, vc_checkpoint_desc(rows, cols, f32, stride), x, kept.q, kept.scales)
+    return kept
+
+
+def checkpoint_unpack(kept, dtype=None, out=None):
+    """The values that checkpoint_pack kept, in the type they had or `dtype`; into `out` where that is given."""
+    import torch
+    q, scales = kept.q, kept.scales
+    rows, cols, _ = _rows_of(q)
+    if out is None:
+        out = torch.empty(q.shape, dtype=kept.dtype if dtype is None else dtype, device=q.device)
+    elif dtype is not None and out.dtype is not dtype:
+        raise ValueError("out must be %s, got %s" % (dtype, out.dtype))
+    f32 = _type("out", out)
+    _check_all([("q", q, q.shape, torch.int8, False),
+                ("scales", scales, q.shape[:-1] + ((cols + BLOCK - 1) // BLOCK,), torch.float32, False),
+                ("out", out, q.shape, out.dtype, False)])
+    if rows:
+        _launch(q.device, vc_checkpoint_unpack, vc_checkpoint_desc(rows, cols, f32, 0), q, scales, out)
+    return out
+
+
+def saved_in_8bit(min_elements=1 << 16):
+    """A context in which autograd keeps activations in 8 bits: tensors of bf16, of at least min_elements elements, two
+    dimensions and 64 columns, that an operation saves for its backward are packed, and unpacked where the backward asks for
+    them. Leaves (parameters, inputs) stay as they are, for they are kept anyway, and so do tensors of 32 bits (log-sum-exps,
+    statistics). An attention's backward then computes its probabilities from the kept q and k."""
+    import torch
+
+    def pack(t):
+        if (t.device.type != "cuda" or t.dtype is not torch.bfloat16 or t.dim() < 2 or
+                t.numel() < min_elements or t.is_leaf or t.shape[-1] < 64 or not t.is_contiguous()):
+            return t
+        return checkpoint_pack(t.detach())
+
+    def unpack(t):
+        return checkpoint_unpack(t) if isinstance(t, Packed8) else t
+
+    return torch.autograd.graph.saved_tensors_hooks(pack, unpack)
+
+
+# --------------------------------------------------------------------------
+# Embedding of tokens
+# --------------------------------------------------------------------------
+
+def _ids(ids):
+    import torch
+    if ids.dtype is not torch.int64 and ids.dtype is not torch.int32:
+        raise ValueError("ids must be torch.int32 or torch.int64, got %s" % ids.dtype)
+    return 1 if ids.dtype is torch.int64 else 0
+
+
+def embedding_fwd(ids, table, scale=1.0, padding_id=None, dtype=None, out=None):
+    """scale * table[ids] of the table's type or `dtype`: ids int32 or int64 of any shape, table [vocab, columns] in bf16 or
+    fp32 (rows may lie further apart). Tokens of the padding id, or of none of the table's, get zeros."""
+    import torch
+    i64, tf = _ids(ids), _type("table", table)
+    if table.dim() != 2:
+        raise ValueError("table has shape %s, expected [vocab, columns]" % (tuple(table.shape),))
+    V, cols = table.shape
+    if out is None:
+        out = torch.empty(ids.shape + (cols,), dtype=table.dtype if dtype is None else dtype, device=table.device)
+    elif dtype is not None and out.dtype is not dtype:
+        raise ValueError("out must be %s, got %s" % (dtype, out.dtype))
+    of = _type("out", out)
+    _check_all([("ids", ids, ids.shape, ids.dtype, False), ("table", table, (V, cols), table.dtype, True),
+                ("out", out, ids.shape + (cols,), out.dtype, False)])
+    desc = vc_embedding_desc(ids.numel(), V, -1 if padding_id is None else padding_id, _row_stride("table", table), cols, i64, tf,
+                             of, scale, 0)
+    if desc.tokens:
+        _launch(table.device, vc_embedding_fwd, desc, ids, table, out)
+    return out
+
+
+def embedding_bwd(dout, ids, vocab, scale=1.0, padding_id=None, dtype=None, into=None, ws=None):
+    """The table's gradient [vocab, columns], of dout's type or `dtype` (bf16 or fp32): scale times the sum of the rows of
+    dout whose tokens have the id, zeros for ids that no token has. into: a gradient that is there, to which the sums are added
+    instead (and which is returned). dout: ids' shape and columns, contiguous or [tokens, columns] with rows further apart."""
+    import torch
+    i64, of = _ids(ids), _type("dout", dout)
+    cols = dout.shape[-1] if dout.dim() else 0
+    if into is None:
+        grad = torch.empty((vocab, cols), dtype=dout.dtype if dtype is None else dtype, device=dout.device)
+    elif dtype is not None and into.dtype is not dtype:
+        raise ValueError("into must be %s, got %s" % (dtype, into.dtype))
+    else:
+        grad = into
+    gf = _type("dtable", grad)
+    _check_all([("dout", dout, ids.shape + (cols,), dout.dtype, True), ("ids", ids, ids.shape, ids.dtype, False),
+                ("into", grad, (vocab, cols), grad.dtype, False)])
+    desc = vc_embedding_desc(ids.numel(), vocab, -1 if padding_id is None else padding_id, _row_stride("dout", dout), cols, i64,
+                             gf, of, scale, 0 if into is None else 1)
+    if not desc.tokens:
+        return grad.zero_() if into is None else grad
+    if ws is None:
+        ws = _workspace(vc_embedding_bwd_workspace_bytes(desc), dout.device)
+    _launch(dout.device, vc_embedding_bwd, desc, ids, dout, grad, ws, _ws_bytes(ws, dout.device))
+    return grad
+
+
+# --------------------------------------------------------------------------
+# Differentiable forms
+# --------------------------------------------------------------------------
+
+_AUTOGRAD = {}
+
+
+def _autograd_functions():
+    if _AUTOGRAD:
+        return _AUTOGRAD
+    import torch
+    from torch.autograd.function import once_differentiable
+
+    class ResidualNorm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, a, gate, scale, shift, post_weight, desc, cu, lens, y_dtype):
+            ctx.set_materialize_grads(False)
+            h, y, s = residual_norm_fwd(x, a, desc, gate, scale, shift, post_weight, cu, lens, y_dtype)
+            kept = (s.h, s.a)
+            if s.desc.checkpoint:
+                kept = tuple(t for k in kept for t in ((None, None) if k is None else (k.q, k.scales)))
+            ctx.save_for_backward(*kept, gate, scale, shift, post_weight, cu, lens, s.mean, s.rstd, s.post_mean, s.post_rstd)
+            ctx.desc, ctx.types = s.desc, (x.dtype, s.y_dtype)
+            if a is None:  # h is x: the caller has it
+                return y
+            return (h, y) if y is not None else h
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, *grads):
+            t, d = ctx.saved_tensors, ctx.desc
+            if d.checkpoint:
+                kept = tuple(None if q is None else Packed8(q, s, dt) for q, s, dt in zip(t[0:4:2], t[1:4:2], ctx.types))
+                t = t[4:]
+            else:
+                kept, t = t[:2], t[2:]
+            dh, dy = grads if len(grads) == 2 else (None, *grads) if kept[1] is None else (*grads, None)
+            if dh is None and dy is None:
+                return (None,) * 10
+            cont = lambda g: None if g is None else g.contiguous()  # noqa: E731
+            saved = ResidualSaved(d, *kept, *t, ctx.types[1])
+            return residual_norm_bwd(cont(dh), cont(dy), saved, want=ctx.needs_input_grad[:6]) + (None,) * 4
+
+    class Embedding(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, ids, table, scale, padding_id, dtype):
+            ctx.save_for_backward(ids)
+            ctx.how = (table.shape[0], scale, padding_id, table.dtype)
+            return embedding_fwd(ids, table, scale, padding_id, dtype)
+
+        @staticmethod
+        @once_differentiable
+        def backward(ctx, dout):
+            return (None, embedding_bwd(dout.contiguous(), ctx.saved_tensors[0], *ctx.how), None, None, None)
+
+    _AUTOGRAD.update(residual=ResidualNorm, embedding=Embedding)
+    return _AUTOGRAD
+
+
+def residual_norm(x, a, desc, gate=None, scale=None, shift=None, post_weight=None, cu=None, lens=None, y_dtype=None):
+    """Differentiable gated residual (see residual_norm_fwd): (h, y) with gradients of x, a, gate, scale, shift and
+    post_weight; y alone without a, h alone where the descriptor has no norm. For a captured graph take residual_norm_fwd and
+    residual_norm_bwd: autograd itself waits, across streams, for other graphs of the same leaves."""
+    return _autograd_functions()["residual"].apply(x, a, gate, scale, shift, post_weight, desc, cu, lens, y_dtype)
+
+
+def embedding(ids, table, scale=1.0, padding_id=None, dtype=None):
+    """Differentiable embedding (see embedding_fwd): the table's gradient has the table's type. For a captured graph take
+    embedding_fwd and embedding_bwd (see residual_norm)."""
+    return _autograd_functions()["embedding"].apply(ids, table, scale, padding_id, dtype)

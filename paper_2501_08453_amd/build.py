@@ -11,8 +11,10 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libvc_jointattn.so")
 SOURCES = ["api.hip", "layout.hip", "fwd.hip", "bwd.hip", "temporal.hip", "temporal_long.hip", "offload.hip",
-           "api_tower.hip", "packed_fwd.hip", "packed_bwd.hip", "norm.hip"]
-HEADERS = ["common.hpp", "host.hpp", "packed.hpp", "norm.hpp"]
+           "api_tower.hip", "packed_fwd.hip", "packed_bwd.hip", "norm.hip", "api_blocks.hip", "residual.hip",
+           "checkpoint.hip", "embedding.hip"]
+HEADERS = ["common.hpp", "host.hpp", "packed.hpp", "norm.hpp", "rows.hpp", "residual.hpp", "checkpoint.hpp",
+           "embedding.hpp"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",
