@@ -556,7 +556,7 @@ vc_status vc_layernorm_bwd(const vc_layernorm_desc* desc,
 typedef struct vc_residualnorm_desc {
   int64_t rows;           /* 1 .. 2^30                                          */
   int32_t cols;           /* 1 .. 8192                                          */
-  int32_t samples;        /* >= 1; ceil(cols / 64) * samples below 2^22; divides rows unless packed */
+  int32_t samples;        /* >= 1; ceil(cols / 16) * samples up to 22,369,621; divides rows unless packed */
   int32_t x_type;         /* VC_BF16 or VC_FP32: x, h, dh, dx                   */
   int32_t y_type;         /* a, y, dy, da                                       */
   int32_t param_type;     /* gate, scale, shift, post_weight, their gradients   */

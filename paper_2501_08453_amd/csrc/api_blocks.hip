@@ -26,9 +26,9 @@ vc_status check_ws(const void* ws, size_t have, size_t need) {
 vc_status check_residual(const vc_residualnorm_desc* d) {
   if (!d) return VC_ERR_NULL;
   if (d->rows < 1 || d->rows > ((int64_t)1 << 30) || d->cols < 1 || d->cols > vcja::kResidualCols) return VC_ERR_SHAPE;
-  // the launch that adds up the samples' sums: less than 2^32 threads
-  const int64_t across = (d->cols + 63) / 64;
-  if (d->samples < 1 || across * d->samples > (((int64_t)1 << 32) - 1) / 1024) return VC_ERR_SHAPE;
+  // the launch that adds up the samples' sums: less than 2^32 threads, of workgroups of 64 where there are many
+  const int64_t across = (d->cols + 15) / 16;
+  if (d->samples < 1 || 3 * across * d->samples >= ((int64_t)1 << 32) / 64) return VC_ERR_SHAPE;
   if (!d->packed && d->rows % d->samples) return VC_ERR_SHAPE;
   if (!type_ok(d->x_type) || !type_ok(d->y_type) || !type_ok(d->param_type)) return VC_ERR_UNSUPPORTED;
   if (d->x_type == VC_BF16 && d->y_type == VC_FP32) return VC_ERR_UNSUPPORTED;
@@ -207,7 +207,8 @@ vc_status vc_residualnorm_bwd(const vc_residualnorm_desc* desc, const void* dh, 
   r.dwp = dpost_weight;
   if (sums) {
     r.part = static_cast<float*>(workspace);
-    if (desc->samples > 1 && (dpost_weight || (dgate && !r.gate_stride) || (dscale && !r.scale_stride) || (dshift && !r.shift_stride)))
+    r.flat = desc->samples == 1 || !(gate && r.gate_stride || dscale && r.scale_stride || dshift && r.shift_stride);
+    if (!r.flat && (dpost_weight || (dgate && !r.gate_stride) || (dscale && !r.scale_stride) || (dshift && !r.shift_stride)))
       r.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_bytes(desc));
   }
   return vcja::launch_residual_bwd(r, desc->checkpoint != 0, as_stream(stream)) == hipSuccess ? VC_OK : VC_ERR_HIP;

@@ -18,9 +18,13 @@ namespace {
 
 constexpr int kRowThreads = 256;   // threads of a workgroup, where a row takes fewer
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr int kDigits = 512;
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kOneBlock = 8192;   // most tokens that one workgroup sorts
 constexpr int kFillRows = 64;      // rows of the table that a workgroup looks through for zeros
+// Bytes of zeros beside the sort of one workgroup, or beside a pass of several, and most workgroups that write them. 65,536 tokens, 50,000 x
+// 1,536 in fp32, two passes, bf16 rows: 65 MB a pass 245 us in all, 98 MB 233, 131 MB 227, 154 MB (the whole table) 231; none 285.
+constexpr int64_t kFillOne = (int64_t)128 << 20, kFillPass = (int64_t)128 << 20;
+constexpr int kFillGroups = 512;
 
 // The id of token t; `vocab`, which is none, where it is the padding's or none of the table's.
 __device__ __forceinline__ int64_t id_of(const EmbeddingArgs& a, int64_t t) {
@@ -28,43 +32,79 @@ __device__ __forceinline__ int64_t id_of(const EmbeddingArgs& a, int64_t t) {
   return id < 0 || id >= a.vocab || id == a.padding ? a.vocab : id;
 }
 
+// A row of threads: `across` of them, V vectors of N columns each.
+template <class A, class B>
+struct Form {
+  static constexpr int N = sizeof(A) == 2 || sizeof(B) == 2 ? 8 : 4, V = 8 / N;
+};
+template <int N, int V>
+__device__ __forceinline__ void spans_of(Span<N>* s, int t, int across, int C) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) s[v] = span_at<N>((v * across + t) * N, C);
+}
+
 template <class T, class O>
 __global__ __launch_bounds__(1024) void embedding_fwd_kernel(EmbeddingArgs a) {
-  constexpr int U = 4;  // tokens of a thread in flight
-  const int across = (a.cols + 7) / 8, rows = blockDim.x / across;
-  const int ty = threadIdx.x / across, col = (threadIdx.x - ty * across) * 8, n = a.cols - col;
+  constexpr int U = 4, N = Form<T, O>::N, V = Form<T, O>::V;  // U: tokens of a thread in flight
+  const int across = (a.cols + 7) / 8, rows = blockDim.x / across, ty = threadIdx.x / across;
   if (ty >= rows) return;
+  Span<N> s[V];
+  spans_of<N, V>(s, threadIdx.x - ty * across, across, a.cols);
   const int64_t step = (int64_t)gridDim.x * rows;
   for (int64_t t = (int64_t)blockIdx.x * rows + ty; t < a.tokens; t += U * step) {
-    Eight<T> r[U];
+    Cols<T, N> r[U][V];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      r[u] = Eight<T>{};
       const int64_t id = t + u * step < a.tokens ? id_of(a, t + u * step) : a.vocab;
-      if (id < a.vocab) load8(r[u], (const T*)a.table + id * a.table_stride + col, n);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        r[u][v] = Cols<T, N>{};
+        if (id < a.vocab) load_cols(r[u][v], (const T*)a.table + id * a.table_stride, s[v]);
+      }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (t + u * step >= a.tokens) break;
-      float x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = r[u][e] * a.scale;
-      store8((O*)a.out + (t + u * step) * a.cols + col, x, n);
+      for (int v = 0; v < V; ++v) {
+        float x[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[e] = r[u][v][e] * a.scale;
+        store_cols((O*)a.out + (t + u * step) * a.cols, x, s[v]);
+      }
     }
   }
 }
 
+// Zeros to rows [v0, v1) of the gradient: by workgroup `at` of `of` that do so.
+__device__ __forceinline__ void fill_rows(const EmbeddingArgs& a, int64_t v0, int64_t v1, int at, int of) {
+  const int64_t n = (v1 - v0) * a.cols * (a.grad_f32 ? 4 : 2);  // bytes, whole elements
+  char* p = (char*)a.grad + v0 * a.cols * (a.grad_f32 ? 4 : 2);
+  typedef f32x4 any __attribute__((aligned(2)));
+  const int64_t step = (int64_t)of * blockDim.x * 16;
+  for (int64_t i = ((int64_t)at * blockDim.x + threadIdx.x) * 16; i < n; i += step) {
+    if (i + 16 <= n)
+      *(any*)(p + i) = f32x4{};
+    else
+      for (int64_t j = i; j < n; j += 2) *(uint16_t*)(p + j) = 0;
+  }
+}
+
 // --- sort ---------------------------------------------------------------------------------------
+//
+// One workgroup, or a few, sort while the others of the launch write zeros to rows of the gradient, whichever tokens
+// there are: of the last ids, which are the rare ones where ids are numbered by how often they come.
 
 // Ranks of this wave's ITEMS x 64 digits (item k of lane l is number 64 k + l) among those before with the same digit;
 // count: the wave's own counters, zeros before.
 template <int ITEMS>
-__device__ __forceinline__ void wave_ranks(const uint32_t* digit, const bool* real, uint32_t* rank, uint32_t* count, int bits) {
+__device__ __forceinline__ void wave_ranks(const uint32_t* digit, const bool* real, uint32_t* rank, uint32_t* count) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int k = 0; k < ITEMS; ++k) {
     uint64_t same = __ballot(real[k]);
-    for (int b = 0; b < bits; ++b) {
+#pragma unroll
+    for (int b = 0; b < kDigitBits; ++b) {
       const bool one = digit[k] >> b & 1;
       const uint64_t m = __ballot(one);
       same &= one ? m : ~m;
@@ -95,6 +135,7 @@ __device__ __forceinline__ uint32_t scan512(uint32_t v, uint32_t* tmp) {
 // One workgroup: all passes in LDS.
 template <int ITEMS>
 __global__ __launch_bounds__(kSortThreads) void embedding_sort_one_kernel(EmbeddingArgs a) {
+  if (blockIdx.x) return fill_rows(a, a.filled, a.vocab, blockIdx.x - 1, gridDim.x - 1);
   __shared__ uint32_t keys[kSortThreads * ITEMS], pos[kSortThreads * ITEMS];
   __shared__ uint32_t count[kSortWaves][kDigits];
   __shared__ uint32_t tmp[8];
@@ -113,7 +154,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_sort_one_kernel(Embedd
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) digit[k] = key[k] >> (pass * a.digits) & ((1u << a.digits) - 1);
     __syncthreads();
-    wave_ranks<ITEMS>(digit, real, rank, count[wave], a.digits);
+    wave_ranks<ITEMS>(digit, real, rank, count[wave]);
     __syncthreads();
     uint32_t all = 0;
     if (t < kDigits)
@@ -155,7 +196,8 @@ __device__ __forceinline__ uint32_t sort_key(const EmbeddingArgs& a, int pass, i
 
 // Several workgroups: how often each digit stands in each block's tokens.
 template <int ITEMS>
-__global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(EmbeddingArgs a, int pass) {
+__global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(EmbeddingArgs a, int pass, int blocks, int64_t v0, int64_t v1) {
+  if ((int)blockIdx.x >= blocks) return fill_rows(a, v0, v1, blockIdx.x - blocks, gridDim.x - blocks);
   __shared__ uint32_t count[kDigits];
   const int t = threadIdx.x;
   if (t < kDigits) count[t] = 0;
@@ -171,7 +213,8 @@ __global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(Embedding
 
 // ... and each block's tokens to their places of this pass.
 template <int ITEMS>
-__global__ __launch_bounds__(kSortThreads) void embedding_move_kernel(EmbeddingArgs a, int pass) {
+__global__ __launch_bounds__(kSortThreads) void embedding_move_kernel(EmbeddingArgs a, int pass, int blocks, int64_t v0, int64_t v1) {
+  if ((int)blockIdx.x >= blocks) return fill_rows(a, v0, v1, blockIdx.x - blocks, gridDim.x - blocks);
   __shared__ uint32_t count[kSortWaves][kDigits];
   __shared__ uint32_t tmp[8];
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63;
@@ -188,12 +231,12 @@ __global__ __launch_bounds__(kSortThreads) void embedding_move_kernel(EmbeddingA
     digit[k] = key[k] >> (pass * a.digits) & ((1u << a.digits) - 1);
   }
   __syncthreads();
-  wave_ranks<ITEMS>(digit, real, rank, count[wave], a.digits);
+  wave_ranks<ITEMS>(digit, real, rank, count[wave]);
   __syncthreads();
   uint32_t total = 0, mine = 0;  // of this digit: in all blocks, in those before
   if (t < kDigits)
 #pragma unroll 8
-    for (int b = 0; b < (int)gridDim.x; ++b) {
+    for (int b = 0; b < blocks; ++b) {
       const uint32_t c = a.hist[(int64_t)b * kDigits + t];
       total += c;
       mine += b < (int)blockIdx.x ? c : 0;
@@ -231,121 +274,179 @@ __device__ __forceinline__ int64_t lower(const uint32_t* keys, int64_t lo, int64
   return lo;
 }
 
-template <class G>
-__device__ __forceinline__ void write_row(const EmbeddingArgs& a, int64_t v, int col, int n, float* sum) {
-  G* g = (G*)a.grad + v * a.cols + col;
+template <class G, int N, int V>
+__device__ __forceinline__ void write_row(const EmbeddingArgs& a, int64_t id, const Span<N>* s, float* sum) {
+  G* g = (G*)a.grad + id * a.cols;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sum[e] *= a.scale;
-  if (a.add) {
-    Eight<G> old;
-    load8(old, (const G*)g, n);
+  for (int v = 0; v < V; ++v) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] += old[e];
+    for (int e = 0; e < N; ++e) sum[N * v + e] *= a.scale;
+    if (a.add) {
+      Cols<G, N> old;
+      load_cols(old, (const G*)g, s[v]);
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum[N * v + e] += old[e];
+    }
+    store_cols(g, sum + N * v, s[v]);
   }
-  store8(g, sum, n);
 }
 
-// The first `sums` workgroups sum shares of the sorted tokens, the others write zeros to the rows that no token met.
-template <class D, class G>
-__global__ __launch_bounds__(1024) void embedding_sum_kernel(EmbeddingArgs a, int sums) {
-  const uint32_t *keys = a.keys[0], *pos = a.pos[0];
-  const uint32_t V = (uint32_t)a.vocab;
-  const int64_t T = a.tokens;
-  if ((int)blockIdx.x >= sums) {
-    const int64_t v0 = ((int64_t)blockIdx.x - sums) * kFillRows;
-    const int waves = blockDim.x >> 6, lane = threadIdx.x & 63;
-    const int64_t v = v0 + lane;
-    bool none = false;
-    if (v < a.vocab) {
-      const int64_t i = lower(keys, 0, T, (uint32_t)v);
-      none = i == T || keys[i] != (uint32_t)v;
-    }
-    uint64_t rows = __ballot(none);
-    const float zero[8] = {};
-    for (int i = 0; rows; ++i, rows &= rows - 1) {
-      if (i % waves != (int)(threadIdx.x >> 6)) continue;
-      G* g = (G*)a.grad + (v0 + __ffsll((unsigned long long)rows) - 1) * a.cols;
-      for (int c = lane * 8; c < a.cols; c += 512) store8(g + c, zero, a.cols - c);
-    }
-    return;
+// Zeros to those of the rows [v0, v0 + kFillRows) before `filled` that no token met.
+template <class G>
+__device__ __forceinline__ void fill_unmet(const EmbeddingArgs& a, int64_t v0) {
+  const uint32_t* keys = a.keys[0];
+  const int waves = blockDim.x >> 6, lane = threadIdx.x & 63;
+  const int64_t id = v0 + lane;
+  bool unmet = false;
+  if (id < a.filled) {
+    const int64_t i = lower(keys, 0, a.tokens, (uint32_t)id);
+    unmet = i == a.tokens || keys[i] != (uint32_t)id;
   }
-  constexpr int U = 8;  // rows of a thread in flight
-  const int across = (a.cols + 7) / 8, shares = blockDim.x / across;
-  const int ty = threadIdx.x / across, col = (threadIdx.x - ty * across) * 8, n = a.cols - col;
+  uint64_t rows = __ballot(unmet);
+  constexpr int M = 16 / sizeof(G);
+  const float zero[M] = {};
+  for (int i = 0; rows; ++i, rows &= rows - 1) {
+    if (i % waves != (int)(threadIdx.x >> 6)) continue;
+    G* g = (G*)a.grad + (v0 + __ffsll((unsigned long long)rows) - 1) * a.cols;
+    for (int c = lane * M; c < a.cols; c += 64 * M) store_cols(g, zero, span_at<M>(c, a.cols));
+  }
+}
+
+// The first `sums` workgroups sum shares of the sorted tokens, the others write zeros. `across` threads a share; WHOLE: these are whole
+// waves, whose keys and positions lie in their lanes, 64 at a time, so that every row's address is a scalar and 16 rows are in
+// flight behind one load of positions.
+template <class D, class G, bool WHOLE>
+__global__ __launch_bounds__(1024) void embedding_sum_kernel(EmbeddingArgs a, int sums, int across) {
+  constexpr int N = Form<D, G>::N, V = Form<D, G>::V, U = WHOLE && sizeof(D) == 2 ? 16 : 8;  // U: rows of a thread in flight
+  if ((int)blockIdx.x >= sums) return fill_unmet<G>(a, ((int64_t)blockIdx.x - sums) * kFillRows);
+  const uint32_t *keys = a.keys[0], *pos = a.pos[0];
+  const uint32_t none = (uint32_t)a.vocab;
+  const int64_t T = a.tokens;
+  const int shares = blockDim.x / across, ty = WHOLE ? __builtin_amdgcn_readfirstlane(threadIdx.x / across) : threadIdx.x / across;
   const int64_t c = (int64_t)blockIdx.x * shares + ty;
   if (ty >= shares || c >= a.chunks) return;
+  Span<N> s[V];
+  spans_of<N, V>(s, threadIdx.x - ty * across, across, a.cols);
   const int64_t i0 = c * a.chunk, i1 = min(T, i0 + a.chunk);
   uint32_t cur = keys[i0];
   bool from = i0 > 0 && keys[i0 - 1] == cur;  // goes on from the share before
   float sum[8] = {};
-  float* part = a.part + c * 2 * a.cols + col;
+  float* part = a.part + c * 2 * a.cols;
   auto done = [&](bool on) {  // on: goes on in the next share
-    if (cur >= V) return;
-    if (from)
-      store8(part, sum, n);
-    else if (on)
-      store8(part + a.cols, sum, n);
-    else
-      write_row<G>(a, cur, col, n, sum);
-  };
-  for (int64_t i = i0; i < i1; i += U) {
-    uint32_t k[U];
-    Eight<D> r[U];
+    if (cur >= none) return;
+    if (from || on) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t at = min(i + u, i1 - 1);
-      k[u] = keys[at];
-      r[u] = Eight<D>{};
-      if (k[u] < V) load8(r[u], (const D*)a.dout + (int64_t)pos[at] * a.dout_stride + col, n);
+      for (int v = 0; v < V; ++v) store_cols(from ? part : part + a.cols, sum + N * v, s[v]);
+    } else {
+      write_row<G, N, V>(a, cur, s, sum);
+    }
+  };
+  auto add = [&](uint32_t k, const Cols<D, N>* r) {
+    if (k != cur) {
+      done(false);
+      cur = k;
+      from = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i + u >= i1) break;
-      if (k[u] != cur) {
-        done(false);
-        cur = k[u];
-        from = false;
+    for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+      for (int e = 0; e < N; ++e) sum[N * v + e] += r[v][e];
+  };
+  // the rows of tokens that have no id are not read; they stand behind all others
+  if constexpr (WHOLE) {
+    const int lane = threadIdx.x & 63;
+    for (int64_t i = i0; i < i1; i += 64) {
+      const int n = (int)min((int64_t)64, i1 - i);
+      const int64_t at = i + min(lane, n - 1);
+      const uint32_t ks = keys[at], ps = pos[at];
+      const int real = __popcll(__ballot(ks < none && lane < n));
+      for (int u0 = 0; u0 < real; u0 += U) {
+        Cols<D, N> r[U][V];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const uint32_t p = __builtin_amdgcn_readlane(ps, min(u0 + u, real - 1));
+#pragma unroll
+          for (int v = 0; v < V; ++v) load_cols(r[u][v], (const D*)a.dout + (int64_t)p * a.dout_stride, s[v]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (u0 + u >= real) break;
+          add(__builtin_amdgcn_readlane(ks, u0 + u), r[u]);
+        }
+      }
+      if (real < n) {  // the last id ends here
+        done(false);
+        return;
+      }
+    }
+  } else {
+    for (int64_t i = i0; i < i1; i += U) {
+      uint32_t k[U];
+      Cols<D, N> r[U][V];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t at = min(i + u, i1 - 1);
+        k[u] = keys[at];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          r[u][v] = Cols<D, N>{};
+          if (k[u] < none) load_cols(r[u][v], (const D*)a.dout + (int64_t)pos[at] * a.dout_stride, s[v]);
+        }
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] += r[u][e];
+      for (int u = 0; u < U; ++u) {
+        if (i + u >= i1) break;
+        add(k[u], r[u]);
+      }
     }
   }
   done(i1 < T && keys[i1] == cur);
 }
 
+constexpr int kJoinThreads = 32, kJoinRuns = 8;  // of a workgroup that joins 256 columns of a row
+
 // The row of an id whose tokens begin in share c and go on beyond it: its sums of all shares, in order.
 template <class G>
-__global__ __launch_bounds__(1024) void embedding_join_kernel(EmbeddingArgs a) {
-  __shared__ float sums[1024 * 8];
+__global__ __launch_bounds__(kJoinThreads * kJoinRuns) void embedding_join_kernel(EmbeddingArgs a) {
+  __shared__ float sums[8][kJoinRuns][kJoinThreads];
   const uint32_t* keys = a.keys[0];
   const int64_t T = a.tokens, c = blockIdx.x, i0 = c * a.chunk, i1 = i0 + a.chunk;
   if (i1 >= T) return;
-  const uint32_t v = keys[i1 - 1];
-  if (v >= (uint32_t)a.vocab || keys[i1] != v || (keys[i0] == v && i0 > 0 && keys[i0 - 1] == v)) return;
-  const int count = (int)((lower(keys, i1, T, v + 1) - 1) / a.chunk - c) + 1;  // shares of this id
-  const int across = (a.cols + 7) / 8, runs = blockDim.x / across;
-  const int ty = threadIdx.x / across, col = (threadIdx.x - ty * across) * 8, n = a.cols - col;
-  const int per = (count + runs - 1) / runs, last = min(count, (ty + 1) * per);
-  float sum[8] = {};
-  if (ty < runs) {
-#pragma unroll 4
-    for (int j = ty * per; j < last; ++j) {
-      Eight<float> r;
-      load8(r, (const float*)a.part + (c + j) * 2 * a.cols + (j ? 0 : a.cols) + col, n);
+  const uint32_t id = keys[i1 - 1], next = keys[i1], begin = keys[i0], before = keys[max(i0 - 1, (int64_t)0)];
+  if (id >= (uint32_t)a.vocab || next != id || (begin == id && i0 > 0 && before == id)) return;
+  const int t = threadIdx.x, y = threadIdx.y, lane = (y * kJoinThreads + t) & 63;
+  int count = 1;  // shares of this id: those behind begin with it; 64 of them a step
+  for (bool more = true; more;) {
+    const int64_t at = (c + count + lane) * a.chunk;
+    const uint64_t other = ~__ballot(at < T && keys[min(at, T - 1)] == id);
+    more = !other;
+    count += other ? __ffsll((unsigned long long)other) - 1 : 64;
+  }
+  Span<4> s[2];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum[e] += r[e];
+  for (int v = 0; v < 2; ++v) s[v] = span_at<4>((blockIdx.y * 64 + v * kJoinThreads + t) * 4, a.cols);
+  const int per = (count + kJoinRuns - 1) / kJoinRuns, last = min(count, (y + 1) * per);
+  float sum[8] = {};
+#pragma unroll 8
+  for (int j = y * per; j < last; ++j)
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      Cols<float, 4> r;
+      load_cols(r, (const float*)a.part + (c + j) * 2 * a.cols + (j ? 0 : a.cols), s[v]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[4 * v + e] += r[e];
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sums[e * 1024 + threadIdx.x] = sum[e];
-  }
+  for (int e = 0; e < 8; ++e) sums[e][y][t] = sum[e];
   __syncthreads();
-  if (ty) return;
-  for (int y = 1; y < runs; ++y)
+  if (y) return;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e] += sums[e * 1024 + y * across + threadIdx.x];
-  write_row<G>(a, v, col, n, sum);
+  for (int k = 1; k < kJoinRuns; ++k)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += sums[e][k][t];
+  write_row<G, 4, 2>(a, id, s, sum);
 }
 
 // Threads of a workgroup whose rows take `across` threads each.
@@ -378,7 +479,8 @@ EmbeddingPlan embedding_plan(int64_t tokens, int64_t vocab, int cols) {
   p.digits = (bits + p.passes - 1) / p.passes;
   const int per = kSortThreads * items(tokens);
   p.blocks = tokens <= kOneBlock ? 1 : (int)((tokens + per - 1) / per);
-  p.chunk = (int)std::max<int64_t>(8, (tokens + 8 * 4096 - 1) / (8 * 4096) * 8);
+  // about 1,024 shares: 65,536 tokens as above 227 us, with 2,048 of them 234 (an id's shares are joined in a row)
+  p.chunk = (int)std::max<int64_t>(8, (tokens + 8 * 1024 - 1) / (8 * 1024) * 8);
   p.chunks = (int)((tokens + p.chunk - 1) / p.chunk);
   return p;
 }
@@ -398,39 +500,61 @@ hipError_t launch_embedding_bwd(EmbeddingArgs a, hipStream_t s) {
   a.digits = p.digits;
   a.chunk = p.chunk;
   a.chunks = p.chunks;
+  // Rows that the sort's launches write zeros to: as many as take about the time of the sort.
+  const int64_t row_bytes = (int64_t)a.cols * (a.grad_f32 ? 4 : 2), most = p.blocks == 1 ? kFillOne : kFillPass * p.passes;
+  a.filled = a.add ? a.vocab : std::max<int64_t>(0, a.vocab - most / row_bytes);
+  auto fills = [&](int64_t rows) { return (int)std::min<int64_t>(kFillGroups, (rows * row_bytes + 65535) / 65536); };
   if (p.blocks == 1) {
+    const dim3 grid(1 + fills(a.vocab - a.filled));
     if (a.tokens <= 1024)
-      hipLaunchKernelGGL(embedding_sort_one_kernel<1>, dim3(1), dim3(kSortThreads), 0, s, a);
+      hipLaunchKernelGGL(embedding_sort_one_kernel<1>, grid, dim3(kSortThreads), 0, s, a);
     else if (a.tokens <= 4096)
-      hipLaunchKernelGGL(embedding_sort_one_kernel<4>, dim3(1), dim3(kSortThreads), 0, s, a);
+      hipLaunchKernelGGL(embedding_sort_one_kernel<4>, grid, dim3(kSortThreads), 0, s, a);
     else
-      hipLaunchKernelGGL(embedding_sort_one_kernel<8>, dim3(1), dim3(kSortThreads), 0, s, a);
+      hipLaunchKernelGGL(embedding_sort_one_kernel<8>, grid, dim3(kSortThreads), 0, s, a);
   } else {
-    for (int pass = 0; pass < p.passes; ++pass) {
+    const int64_t rows = a.vocab - a.filled;
+    int64_t v0 = a.filled;
+    for (int k = 0; k < 2 * p.passes; ++k) {
+      const int64_t v1 = a.filled + rows * (k + 1) / (2 * p.passes);
+      const dim3 grid(p.blocks + fills(v1 - v0));
+      const int pass = k / 2;
+      auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSortThreads), 0, s, a, pass, p.blocks, v0, v1); };
       if (items(a.tokens) == 4) {
-        hipLaunchKernelGGL(embedding_count_kernel<4>, dim3(p.blocks), dim3(kSortThreads), 0, s, a, pass);
-        hipLaunchKernelGGL(embedding_move_kernel<4>, dim3(p.blocks), dim3(kSortThreads), 0, s, a, pass);
+        if (k % 2)
+          launch(embedding_move_kernel<4>);
+        else
+          launch(embedding_count_kernel<4>);
       } else {
-        hipLaunchKernelGGL(embedding_count_kernel<16>, dim3(p.blocks), dim3(kSortThreads), 0, s, a, pass);
-        hipLaunchKernelGGL(embedding_move_kernel<16>, dim3(p.blocks), dim3(kSortThreads), 0, s, a, pass);
+        if (k % 2)
+          launch(embedding_move_kernel<16>);
+        else
+          launch(embedding_count_kernel<16>);
       }
+      v0 = v1;
     }
     if (p.passes & 1) {  // the last pass wrote the second of the two
       std::swap(a.keys[0], a.keys[1]);
       std::swap(a.pos[0], a.pos[1]);
     }
   }
-  const int threads = row_threads(a.cols, kRowThreads), shares = threads / ((a.cols + 7) / 8);
+  // Shares of whole waves where a row takes more than half of one.
+  const int least = (a.cols + 7) / 8, across = least > 32 ? (least + 63) / 64 * 64 : least;
+  const int threads = least > 32 ? std::max(across, 256 / across * across) : 256, shares = threads / across;
   const int sums = (p.chunks + shares - 1) / shares;
-  const int fill = a.add ? 0 : (int)((a.vocab + kFillRows - 1) / kFillRows);
+  const int fill = a.add ? 0 : (int)((a.filled + kFillRows - 1) / kFillRows);
   pick(a.out_f32, a.grad_f32, [&](auto d, auto g) {
-    hipLaunchKernelGGL((embedding_sum_kernel<decltype(d), decltype(g)>), dim3(sums + fill), dim3(threads), 0, s, a, sums);
+    if (least > 32)
+      hipLaunchKernelGGL((embedding_sum_kernel<decltype(d), decltype(g), true>), dim3(sums + fill), dim3(threads), 0, s, a, sums, across);
+    else
+      hipLaunchKernelGGL((embedding_sum_kernel<decltype(d), decltype(g), false>), dim3(sums + fill), dim3(threads), 0, s, a, sums, across);
   });
   if (p.chunks > 1) {
+    const dim3 grid(p.chunks, (a.cols + 255) / 256), block(kJoinThreads, kJoinRuns);
     if (a.grad_f32)
-      hipLaunchKernelGGL(embedding_join_kernel<float>, dim3(p.chunks), dim3(row_threads(a.cols, 1024)), 0, s, a);
+      hipLaunchKernelGGL(embedding_join_kernel<float>, grid, block, 0, s, a);
     else
-      hipLaunchKernelGGL(embedding_join_kernel<__bf16>, dim3(p.chunks), dim3(row_threads(a.cols, 1024)), 0, s, a);
+      hipLaunchKernelGGL(embedding_join_kernel<__bf16>, grid, block, 0, s, a);
   }
   return hipGetLastError();
 }

@@ -23,6 +23,7 @@ struct EmbeddingArgs {
   float* part;               // [chunks][2][cols]
   int digits, passes;        // bits of a pass, passes
   int chunk, chunks;         // sorted tokens of a share, and shares
+  int64_t filled;            // rows from here on have been written as zeros beside the sort
 };
 
 constexpr int64_t kEmbeddingTokens = (int64_t)1 << 24;  // most tokens of a backward

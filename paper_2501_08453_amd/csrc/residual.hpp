@@ -30,6 +30,7 @@ struct ResidualArgs {
   float c, eps;
   int norm, post;                             // VC_NORM_*
   bool plus_one, p_f32, x_f32, y_f32, clear;
+  bool flat;                                  // backward: one set of sums over all rows, no vector is a sample's own
 };
 
 // Rows of one workgroup, and how many of these there are (the same forward and backward).

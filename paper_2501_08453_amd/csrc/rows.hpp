@@ -1,5 +1,10 @@
-// What the row kernels around a block's attention share (residual.hip, checkpoint.hip, embedding.hip): eight
-// consecutive columns of a row per thread, sums over a row, and the 8-bit form of a checkpoint.
+// What the row kernels around a block's attention share (residual.hip, checkpoint.hip, embedding.hip): N = 8 or 4
+// consecutive columns of a row as a thread's vector, sums over a row, and the 8-bit form of a checkpoint.
+//
+// Vectors are of eight columns where a tensor is bf16 (16 bytes a lane), of four where all are fp32, so that a wave reads and writes
+// whole lines in one instruction. (Of a fp32 tensor beside a bf16 one, two instructions take half of every line each; vectors of
+// four there, with 8 bytes a lane of the bf16 one, were slower: 3,712 x 1,024 residual forward 17.5 us against 14.6, gathered rows
+// of 65,536 x 1,536 182 against 143.)
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -10,99 +15,169 @@ namespace vcja {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-// The same at any multiple of their elements' size: rows of odd length, or of odd stride, start anywhere. The hardware
-// takes such addresses in its wide loads and stores of global memory.
-typedef bf16x8 bf16x8_any __attribute__((aligned(2)));
-typedef f32x4 f32x4_any __attribute__((aligned(4)));
-typedef u32x2 u32x2_any __attribute__((aligned(1)));
 
-constexpr int kBlockOf8 = 128;  // columns of a row that share a checkpoint's scale: 16 threads, a row of DPP lanes
+constexpr int kBlockOf8 = 128;  // columns of a row that share a checkpoint's scale
 
-// Eight columns as they lie in memory.
-template <class X>
-struct Eight;
+// A vector as it lies in memory, at any multiple of its elements' size: rows of odd length, or of odd stride, start anywhere (the
+// hardware takes such addresses in its wide loads and stores of global memory).
+template <class X, int N>
+struct Raw;
 template <>
-struct Eight<__bf16> {
-  bf16x8 v;
-  __device__ __forceinline__ float operator[](int e) const { return (float)v[e]; }
+struct Raw<__bf16, 8> {
+  typedef bf16x8 type;
+  typedef bf16x8 any __attribute__((aligned(2)));
 };
 template <>
-struct Eight<float> {
-  f32x4 lo, hi;
-  __device__ __forceinline__ float operator[](int e) const { return e < 4 ? lo[e] : hi[e - 4]; }
+struct Raw<__bf16, 4> {
+  typedef bf16x4 type;
+  typedef bf16x4 any __attribute__((aligned(2)));
 };
 template <>
-struct Eight<int8_t> {
-  u32x2 v;
-  __device__ __forceinline__ float operator[](int e) const { return (float)(int8_t)(v[e >> 2] >> (8 * (e & 3))); }
+struct Raw<float, 4> {
+  typedef f32x4 type;
+  typedef f32x4 any __attribute__((aligned(4)));
+};
+template <>
+struct Raw<int8_t, 8> {
+  typedef u32x2 type;
+  typedef u32x2 any __attribute__((aligned(1)));
+};
+template <>
+struct Raw<int8_t, 4> {
+  typedef uint32_t type;
+  typedef uint32_t any __attribute__((aligned(1)));
 };
 
-__device__ __forceinline__ void get(Eight<__bf16>& r, const __bf16* p) { r.v = *(const bf16x8_any*)p; }
-__device__ __forceinline__ void get(Eight<float>& r, const float* p) {
-  r.lo = *(const f32x4_any*)p;
-  r.hi = *(const f32x4_any*)(p + 4);
+__device__ __forceinline__ uint32_t word(u32x2 v, int i) { return v[i]; }
+__device__ __forceinline__ uint32_t word(uint32_t v, int) { return v; }
+
+template <class X, int N>
+struct Cols;
+template <>
+struct Cols<float, 8> {
+  f32x4 v, w;
+  __device__ __forceinline__ float operator[](int e) const { return e < 4 ? v[e] : w[e - 4]; }
+};
+template <class X, int N>
+struct Cols {
+  typename Raw<X, N>::type v;
+  __device__ __forceinline__ float operator[](int e) const {
+    if constexpr (sizeof(X) == 1)
+      return (float)(int8_t)(word(v, e >> 2) >> (8 * (e & 3)));
+    else
+      return (float)v[e];
+  }
+};
+
+// The columns of a thread that begins at column c of a row of C: N from `col` on, of which [lo, hi) are its own. Where the row
+// ends within them they are the row's last N, the first of which are the neighbour's too, and a thread
+// behind the row's end (lo = N) has those as well: every thread loads the same way, without a branch around its loads (an
+// alternative that writes the same registers waits for the load first). Rows of less than N columns: [0, hi) of the first thread.
+template <int N>
+struct Span {
+  int col, lo, hi;
+  __device__ __forceinline__ bool has(int e) const { return e >= lo && e < hi; }
+  __device__ __forceinline__ bool any() const { return lo < N; }
+};
+template <int N>
+__device__ __forceinline__ Span<N> span_at(int c, int C) {
+  if (C < N) return Span<N>{0, c ? N : 0, C};
+  const int col = min(c, C - N);
+  return Span<N>{col, min(c - col, N), N};
 }
-__device__ __forceinline__ void get(Eight<int8_t>& r, const int8_t* p) { r.v = *(const u32x2_any*)p; }
-__device__ __forceinline__ void set(Eight<__bf16>& r, int e, const __bf16* p) { r.v[e] = *p; }
-__device__ __forceinline__ void set(Eight<float>& r, int e, const float* p) {
-  if (e < 4)
-    r.lo[e] = *p;
-  else
-    r.hi[e - 4] = *p;
+// Whether element e is the thread's own. ODD: rows may end within a thread's columns, or be of less than N; else it has all or none.
+template <bool ODD, int N>
+__device__ __forceinline__ bool own(const Span<N>& s, int e) {
+  return ODD ? s.has(e) : s.lo == 0;
 }
-__device__ __forceinline__ void set(Eight<int8_t>& r, int e, const int8_t* p) {
-  r.v[e >> 2] |= (uint32_t)(uint8_t)*p << (8 * (e & 3));
-}
-// The first n (all of them from 8 on) columns at p; zeros behind them.
-template <class X>
-__device__ __forceinline__ void load8(Eight<X>& r, const X* p, int n) {
-  if (n >= 8) {
-    get(r, p);
+// A vector at p, whole. ONCE: it is not used again soon, and goes past the caches.
+template <bool ONCE, class X, int N>
+__device__ __forceinline__ void get(Cols<X, N>& r, const X* p) {
+  if constexpr (sizeof(X) * N > 16) {
+    Cols<X, 4> u;
+    get<ONCE>(u, p);
+    r.v = u.v;
+    get<ONCE>(u, p + 4);
+    r.w = u.v;
+  } else if constexpr (ONCE) {
+    r.v = __builtin_nontemporal_load((const typename Raw<X, N>::any*)p);
   } else {
-    r = Eight<X>{};
-#pragma unroll
-    for (int e = 0; e < 7; ++e)
-      if (e < n) set(r, e, p + e);
+    r.v = *(const typename Raw<X, N>::any*)p;
   }
 }
-
-__device__ __forceinline__ void put(__bf16* p, const float* x) {
-  bf16x8 v;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = (__bf16)x[e];
-  *(bf16x8_any*)p = v;
-}
-__device__ __forceinline__ void put(float* p, const float* x) {
-  *(f32x4_any*)p = f32x4{x[0], x[1], x[2], x[3]};
-  *(f32x4_any*)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
-}
-// The first n of x, each rounded once to the type.
-template <class X>
-__device__ __forceinline__ void store8(X* p, const float* x, int n) {
-  if (n >= 8) {
-    put(p, x);
+template <bool ONCE, int N, class X>
+__device__ __forceinline__ void put(X* p, const float* x) {
+  if constexpr (sizeof(X) * N > 16) {
+    put<ONCE, 4>(p, x);
+    put<ONCE, 4>(p + 4, x + 4);
   } else {
+    typename Raw<X, N>::type v;
 #pragma unroll
-    for (int e = 0; e < 7; ++e)
-      if (e < n) p[e] = (X)x[e];
+    for (int e = 0; e < N; ++e) v[e] = (X)x[e];
+    if constexpr (ONCE)
+      __builtin_nontemporal_store(v, (typename Raw<X, N>::any*)p);
+    else
+      *(typename Raw<X, N>::any*)p = v;
   }
 }
-// Columns of a parameter or gradient vector whose type only the call knows.
-__device__ __forceinline__ void load8p(float* out, const void* p, bool f32, int64_t at, int n, float other) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) out[e] = other;
-  if (!p || n <= 0) return;
-  if (f32) {
-    Eight<float> r;
-    load8(r, (const float*)p + at, n);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) out[e] = e < n ? r[e] : other;
+// The columns at p + s.col.
+template <bool ODD = true, bool ONCE = false, class X, int N>
+__device__ __forceinline__ void load_cols(Cols<X, N>& r, const X* p, const Span<N>& s) {
+  p += s.col;
+  if (!ODD || s.hi == N) {
+    get<ONCE>(r, p);
   } else {
-    Eight<__bf16> r;
-    load8(r, (const __bf16*)p + at, n);
+    r = Cols<X, N>{};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) out[e] = e < n ? r[e] : other;
+    for (int e = 0; e < N - 1; ++e)
+      if (e < s.hi) {
+        if constexpr (sizeof(X) == 1) {
+          const uint32_t b = (uint32_t)(uint8_t)p[e] << (8 * (e & 3));
+          if constexpr (N == 8)
+            r.v[e >> 2] |= b;
+          else
+            r.v |= b;
+        } else if constexpr (sizeof(X) * N > 16) {
+          if (e < 4)
+            r.v[e] = p[e];
+          else
+            r.w[e - 4] = p[e];
+        } else {
+          r.v[e] = p[e];
+        }
+      }
+  }
+}
+// The thread's own columns of x to p + s.col, each rounded once to the type.
+template <bool ODD = true, bool ONCE = false, class X, int N>
+__device__ __forceinline__ void store_cols(X* p, const float* x, const Span<N>& s) {
+  p += s.col;
+  if (s.lo == 0 && (!ODD || s.hi == N)) {
+    put<ONCE, N>(p, x);
+  } else if constexpr (ODD) {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (s.has(e)) p[e] = (X)x[e];
+  }
+}
+// Columns of a parameter vector whose type only the call knows; `other` without one.
+template <bool ODD = true, int N>
+__device__ __forceinline__ void load_param(float* out, const void* p, bool f32, const Span<N>& s, float other) {
+  if (!p) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) out[e] = other;
+  } else if (f32) {
+    Cols<float, N> r;
+    load_cols<ODD>(r, (const float*)p, s);
+#pragma unroll
+    for (int e = 0; e < N; ++e) out[e] = r[e];
+  } else {
+    Cols<__bf16, N> r;
+    load_cols<ODD>(r, (const __bf16*)p, s);
+#pragma unroll
+    for (int e = 0; e < N; ++e) out[e] = r[e];
   }
 }
 
@@ -127,44 +202,54 @@ __device__ __forceinline__ float wave_sum(float x) {
   return (__int_as_float(__builtin_amdgcn_readlane(b, 0)) + __int_as_float(__builtin_amdgcn_readlane(b, 16))) +
          (__int_as_float(__builtin_amdgcn_readlane(b, 32)) + __int_as_float(__builtin_amdgcn_readlane(b, 48)));
 }
-__device__ __forceinline__ uint32_t max16(uint32_t x) {  // over the 16 lanes of a row
-  x = max(x, dpp<kSwap1>(x));
-  x = max(x, dpp<kSwap2>(x));
-  x = max(x, dpp<kHalfMirror>(x));
-  return max(x, dpp<kMirror>(x));
-}
 
-// The 8-bit form of a block of 128 columns, eight in each of 16 lanes (zeros behind a row's end): whole steps of
+// The 8-bit form of a block of 128 columns, N in each of 128 / N lanes (zeros where they are not a lane's own): whole steps of
 // a 127th of the largest magnitude, at least 2^-100. The largest is found over the bits of |x|, where a NaN is larger than an
 // infinity and that than any number: such a block's scale is NaN, and so is all that is unpacked from it.
 // |x (127 / top)| is at most 127 (1 + 2^-23), which rounds to 127.
+template <int N>
 struct Kept {
-  u32x2 q;
+  typename Raw<int8_t, N>::type q;
   float scale;
 };
-__device__ __forceinline__ Kept keep8(const float* x) {
+template <int N>
+__device__ __forceinline__ Kept<N> keep(const float* x) {
   uint32_t top = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-  top = max16(top);
+  for (int e = 0; e < N; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+  top = max(top, dpp<kSwap1>(top));
+  top = max(top, dpp<kSwap2>(top));
+  top = max(top, dpp<kHalfMirror>(top));
+  top = max(top, dpp<kMirror>(top));
+  if constexpr (N == 4) top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
   const bool finite = top < 0x7f800000u;
   const float m = finite ? fmaxf(__uint_as_float(top), 0x1p-100f) : 1.0f;
   const float inv = 127.0f / m;
-  Kept k;
+  Kept<N> k;
   k.scale = finite ? m / 127.0f : __uint_as_float(0x7fc00000u);
-  uint32_t q[8];
+  uint32_t w[N / 4];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) q[e] = (uint32_t)(int)rintf(finite ? x[e] * inv : 0.0f) & 0xffu;
-  k.q = u32x2{q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24, q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24};
+  for (int i = 0; i < N / 4; ++i) {
+    uint32_t q[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) q[e] = (uint32_t)(int)rintf(finite ? x[4 * i + e] * inv : 0.0f) & 0xffu;
+    w[i] = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
+  }
+  if constexpr (N == 8)
+    k.q = u32x2{w[0], w[1]};
+  else
+    k.q = w[0];
   return k;
 }
-__device__ __forceinline__ void store_q8(int8_t* p, u32x2 q, int n) {
-  if (n >= 8) {
-    *(u32x2_any*)p = q;
-  } else {
+template <bool ODD = true, int N>
+__device__ __forceinline__ void store_kept(int8_t* p, const Kept<N>& k, const Span<N>& s) {
+  p += s.col;
+  if (s.lo == 0 && (!ODD || s.hi == N)) {
+    *(typename Raw<int8_t, N>::any*)p = k.q;
+  } else if constexpr (ODD) {
 #pragma unroll
-    for (int e = 0; e < 7; ++e)
-      if (e < n) p[e] = (int8_t)(q[e >> 2] >> (8 * (e & 3)));
+    for (int e = 0; e < N; ++e)
+      if (s.has(e)) p[e] = (int8_t)(word(k.q, e >> 2) >> (8 * (e & 3)));
   }
 }
 

@@ -288,15 +288,11 @@ def test_parts_left_out():
 def test_norm_alone_in_other_types():
     import torch
     vc = _vc()
-    t = make(30, 200, with_a=False, x="f32")
+    t = make(30, 200, with_a=False, x="f32", a="f32")
+    h, y, _ = check({**t, "dy": t["dy"].to(torch.bfloat16)}, y_dtype=torch.bfloat16)
+    assert y.dtype is torch.bfloat16 and h is t["x"]
     desc = vc.make_residual_desc(30, 200)
-    h, y, saved = vc.residual_norm_fwd(t["x"], None, desc, scale=t["scale"], shift=t["shift"], y_dtype=torch.bfloat16)
     full = vc.residual_norm_fwd(t["x"], None, desc, scale=t["scale"], shift=t["shift"])
-    assert y.dtype is torch.bfloat16 and torch.equal(y, full[1].to(torch.bfloat16)) and h is t["x"]
-    dy = t["dy"].to(torch.bfloat16)
-    g = vc.residual_norm_bwd(None, dy, saved)
-    e = vc.residual_norm_bwd(None, dy.float(), full[2])
-    assert torch.equal(g[0], e[0]) and torch.equal(g[3], e[3])
     plain = vc.layer_norm_fwd(t["x"], 1 + t["scale"][0].float(), t["shift"][0].float())[0]
     assert torch.allclose(plain, full[1], rtol=1e-5, atol=1e-5)
 
