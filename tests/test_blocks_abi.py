@@ -153,7 +153,7 @@ def test_helpers_check_before_calling():
     cu = torch.zeros(5, dtype=torch.int32)
     d = vc.make_residual_desc(40, 100, 4)
     call = lambda *p, **kw: lambda: vc.residual_norm_fwd(*p, d, **kw)  # noqa: E731
-    saved = vc.ResidualSaved(d, x, a, None, None, None, None, None, None, torch.zeros(40), torch.zeros(40), None, None, torch.bfloat16)
+    saved = vc.ResidualSaved(d, x, a, None, None, None, None, None, None, torch.zeros(4, 40), torch.bfloat16)
     alone = vc.make_residual_desc(40, 100, 4, norm=None)
     ids, table = torch.zeros(9, dtype=torch.int64), bf(30, 16)
     for match, f in (
@@ -178,6 +178,7 @@ def test_helpers_check_before_calling():
             ("dh has shape", lambda: vc.residual_norm_bwd(x[:-1], a, saved)),
             ("no y without a norm", lambda: vc.residual_norm_bwd(None, a, saved._replace(desc=alone))),
             ("x must be torch", lambda: vc.checkpoint_pack(x.half())),
+            ("x has shape", lambda: vc.checkpoint_pack(x[0, 0])),
             ("must be on a GPU", lambda: vc.checkpoint_pack(x)),
             ("out must be", lambda: vc.checkpoint_unpack(vc.Packed8(x, x, x.dtype), dtype=torch.half)),
             ("ids must be torch", lambda: vc.embedding_fwd(ids.short(), table)),

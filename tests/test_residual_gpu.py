@@ -137,8 +137,8 @@ def check(t, norm="layer", post=None, c=1.0, plus_one=True, eps=1e-5, slots=None
             nh, mh, rh = B.normed(hs, norm, eps)
             eh, relh = _stats_err(hs, norm, rh)
             if norm == "layer":
-                _near("mean", saved.mean[r_], mh, eh, worst)
-            _near("rstd", saved.rstd[r_], rh, relh * rh, worst)
+                _near("mean", saved.stats[0, r_], mh, eh, worst)
+            _near("rstd", saved.stats[1, r_], rh, relh * rh, worst)
             e_nh = _normed_err(hs, nh, mh, rh, eh, relh)
             want = B.modulated(hs, e_, f, norm, eps, plus_one)
             tol = e_nh * np.abs(e1) + 4 * U * (np.abs(nh * e1) + np.abs(0 if f is None else f))
