@@ -299,16 +299,23 @@ def _rows_of(x):
     return x.numel() // x.shape[-1], x.shape[-1], _row_stride("x", x)
 
 
-def checkpoint_pack(x):
+def checkpoint_pack(x, out=None):
     """x (bf16 or fp32; contiguous, or [rows, columns] with rows further apart) in 8 bits, a scale for each 128
     columns: a Packed8 of 1 + 1/32 bytes an element. Off by at most half a step, the largest |x| of the 128 over 254; a block
-    that holds an infinity or a NaN unpacks to NaN."""
+    that holds an infinity or a NaN unpacks to NaN. out: a Packed8 of x's shape and type to write to."""
     import torch
     f32 = _type("x", x)
     rows, cols, stride = _rows_of(x)
-    _check_all([("x", x, x.shape, x.dtype, True)])
-    kept = Packed8(torch.empty(x.shape, dtype=torch.int8, device=x.device),
-                   torch.empty(x.shape[:-1] + ((cols + BLOCK - 1) // BLOCK,), dtype=torch.float32, device=x.device), x.dtype)
+    kept, blocks = out, x.shape[:-1] + ((cols + BLOCK - 1) // BLOCK,)
+    if out is None:
+        _check_all([("x", x, x.shape, x.dtype, True)])
+        kept = Packed8(torch.empty(x.shape, dtype=torch.int8, device=x.device),
+                       torch.empty(blocks, dtype=torch.float32, device=x.device), x.dtype)
+    elif out.dtype is not x.dtype:
+        raise ValueError("out is of %s, x of %s" % (out.dtype, x.dtype))
+    else:
+        _check_all([("x", x, x.shape, x.dtype, True), ("out.q", out.q, x.shape, torch.int8, False),
+                    ("out.scales", out.scales, blocks, torch.float32, False)])
     if rows:
         _call_on(x.device, "vc_checkpoint_pack", vc_checkpoint_desc(rows, cols, f32, stride), x, kept.q, kept.scales)
     return kept

@@ -9,20 +9,24 @@ ratio is recomputed (Sec. VI-D, Tab. offload). For the attention of a parallel b
 saved activations are what each branch's backward needs besides q, k, v: its O and LSE
 (the joint, spatial and temporal branches; the branch sum needs nothing).
 
-`plan` assigns every layer keep / recompute / offload; `BlockStack` runs the block's
+A fourth strategy keeps the layers' O in 8 bits on the device (checkpoint_pack; LSE as it is): 1 + 1/32
+bytes an element instead of 2, and D of their backward from values off by up to half a step of a 127th of the
+largest of each 128.
+
+`plan` assigns every layer keep / recompute / offload / pack; `BlockStack` runs the block's
 forward through all layers and the backward in reverse under such a plan, with the
 library's kernels and its offload engine (vc_offload_*). It only schedules calls: every
 step of the computation runs in the library.
 
 Device memory for saved outputs: one set per kept layer, one scratch set shared by the
-recomputed layers, and one set (two when some offloaded layers are adjacent) that the
+recomputed and packed layers (which have their 8 bits and LSE besides), and one set (two when some offloaded layers are adjacent) that the
 offloaded ones use in turn. An offloaded layer's set is stored to pinned host memory right
 after its forward (on the engine's copy stream, overlapping the next layers' forwards) and
 loaded back before its backward (overlapping the backward of a later layer).
 """
 from __future__ import annotations
 
-MODES = ("keep", "recompute", "offload", "combination")
+MODES = ("keep", "recompute", "offload", "combination", "pack")
 OFFLOAD_SHARE = 0.2  # offloaded share in the combination (Sec. VI-D)
 
 
@@ -31,21 +35,21 @@ def _count(share: float, layers: int) -> int:
 
 
 def plan(layers: int, ratio: float, mode: str, offload_share: float = OFFLOAD_SHARE) -> list:
-    """Strategy per layer ("keep", "recompute" or "offload"), in forward order.
+    """Strategy per layer ("keep", "recompute", "offload" or "pack"), in forward order.
 
-    recompute / offload: round(ratio * layers) layers take that strategy;
+    recompute / offload / pack: round(ratio * layers) layers take that strategy;
     combination: round(offload_share * layers) of them (at most the selected count) are
     offloaded and the rest of the selected ones recomputed; keep: none (ratio ignored).
     Offloaded layers come first: every other layer from layer 0 when they are at most half
     of the layers (then one device set holds them in turn: each store overlaps the next
     layer's forward and each load the backward of the layer after it), else the leading
-    ones (two sets in turn). Recomputed layers fill the earliest remaining positions."""
+    ones (two sets in turn). Recomputed (packed) layers fill the earliest remaining positions."""
     if mode not in MODES:
         raise ValueError("mode must be one of %s" % (MODES,))
     if layers < 1 or not 0.0 <= ratio <= 1.0:
         raise ValueError("need layers >= 1 and 0 <= ratio <= 1")
     selected = 0 if mode == "keep" else _count(ratio, layers)
-    if mode == "recompute":
+    if mode == "recompute" or mode == "pack":
         n_off, n_rec = 0, selected
     elif mode == "offload":
         n_off, n_rec = selected, 0
@@ -59,7 +63,7 @@ def plan(layers: int, ratio: float, mode: str, offload_share: float = OFFLOAD_SH
         st[i] = "offload"
     rest = [i for i in range(layers) if st[i] == "keep"]
     for i in rest[:n_rec]:
-        st[i] = "recompute"
+        st[i] = "pack" if mode == "pack" else "recompute"
     return st
 
 
@@ -74,10 +78,10 @@ def ring_size(strategies: list) -> int:
 
 
 def device_sets(strategies: list) -> int:
-    """Saved-output sets held on the device under a plan."""
+    """Saved-output sets held on the device under a plan (packed layers' 8 bits aside)."""
     keep = strategies.count("keep")
-    rec = 1 if "recompute" in strategies else 0
-    return keep + rec + ring_size(strategies)
+    scratch = 1 if "recompute" in strategies or "pack" in strategies else 0
+    return keep + scratch + ring_size(strategies)
 
 
 def ring_slots(strategies: list) -> dict:
@@ -89,7 +93,7 @@ def ring_slots(strategies: list) -> dict:
 
 def forward_ops(strategies: list) -> list:
     """Forward schedule: ("fwd", i) for every layer, ("store", i) after an offloaded
-    layer's forward, and ("wait",) (the stream waits for every copy issued so far) where an
+    layer's forward, ("pack", i) after a packed layer's, and ("wait",) (the stream waits for every copy issued so far) where an
     offloaded forward is about to reuse a set whose store may still run: with one set,
     right before that forward (the store overlapped the layers in between); with two,
     right after the previous offloaded forward (its predecessor's store overlapped it)."""
@@ -99,6 +103,8 @@ def forward_ops(strategies: list) -> list:
         if s == "offload" and ring == 1 and not first:
             ops.append(("wait",))
         ops.append(("fwd", i))
+        if s == "pack":
+            ops.append(("pack", i))
         if s == "offload":
             if ring == 2 and not first:
                 ops.append(("wait",))
@@ -113,7 +119,7 @@ def backward_ops(strategies: list) -> list:
     is not queued yet (the load is ordered after the work queued before it, and issued
     before the current layer's backward so that the two overlap); ("wait",) after that
     backward makes the stream wait for the load; ("recompute", i) re-runs a recomputed
-    layer's forwards before ("bwd", i)."""
+    layer's forwards before ("bwd", i), ("unpack", i) brings a packed one's outputs back."""
     slot = ring_slots(strategies)
     pending = sorted(slot, reverse=True)
     loaded, ops = set(), []
@@ -129,6 +135,8 @@ def backward_ops(strategies: list) -> list:
             ops.append(("load", prefetch))
         if strategies[i] == "recompute":
             ops.append(("recompute", i))
+        elif strategies[i] == "pack":
+            ops.append(("unpack", i))
         ops.append(("bwd", i))
         loaded.discard(i)
         if prefetch is not None:
@@ -169,13 +177,19 @@ class BlockStack:
         self.off_layers = sorted(slots)
         ring = ring_size(self.strategies)
         self.ring = [new_set() for _ in range(ring)]
-        self.scratch = new_set() if "recompute" in self.strategies else None
+        self.scratch = new_set() if "recompute" in self.strategies or "pack" in self.strategies else None
+        cols = -(-D // 128)  # blocks of a head's columns
+        self.packed = {i: [vc.Packed8(torch.empty(q.shape, dtype=torch.int8, device=dev),
+                                      torch.empty((B, N, H, cols), dtype=torch.float32, device=dev), q.dtype)
+                           for _ in range(3)] for i, s in enumerate(self.strategies) if s == "pack"}
         self.sets = []
         for i, s in enumerate(self.strategies):
             if s == "keep":
                 self.sets.append(new_set())
             elif s == "recompute":
                 self.sets.append(self.scratch)
+            elif s == "pack":  # an LSE of its own
+                self.sets.append([torch.empty_like(t) if j % 2 else t for j, t in enumerate(self.scratch)])
             else:
                 self.sets.append(self.ring[slots[i]])
         self.host = {i: [torch.empty(t.shape, dtype=t.dtype, pin_memory=True) for t in self.ring[0]]
@@ -212,6 +226,18 @@ class BlockStack:
         for h, t in zip(self.host[i], self.sets[i]):
             self.off.load(t, h, stream)
 
+    def _pack(self, i, stream):
+        import torch
+        with torch.cuda.stream(stream):
+            for kept, o in zip(self.packed[i], self.sets[i][::2]):
+                self.vc.checkpoint_pack(o, out=kept)
+
+    def _unpack(self, i, stream):
+        import torch
+        with torch.cuda.stream(stream):
+            for kept, o in zip(self.packed[i], self.sets[i][::2]):
+                self.vc.checkpoint_unpack(kept, out=o)
+
     # -- whole stack ----------------------------------------------------------------
     def _run(self, ops, douts, stream):
         for op in ops:
@@ -220,6 +246,10 @@ class BlockStack:
                 self._forward(op[1], stream)
             elif kind == "bwd":
                 self._backward(op[1], douts[op[1]], stream)
+            elif kind == "pack":
+                self._pack(op[1], stream)
+            elif kind == "unpack":
+                self._unpack(op[1], stream)
             elif kind == "store":
                 self._store(op[1], stream)
             elif kind == "load":

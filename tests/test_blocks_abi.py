@@ -180,6 +180,8 @@ def test_helpers_check_before_calling():
             ("x must be torch", lambda: vc.checkpoint_pack(x.half())),
             ("x has shape", lambda: vc.checkpoint_pack(x[0, 0])),
             ("must be on a GPU", lambda: vc.checkpoint_pack(x)),
+            ("out is of", lambda: vc.checkpoint_pack(x, out=vc.Packed8(x, x, torch.float32))),
+            ("out.q must be", lambda: vc.checkpoint_pack(x, out=vc.Packed8(x, x, x.dtype))),
             ("out must be", lambda: vc.checkpoint_unpack(vc.Packed8(x, x, x.dtype), dtype=torch.half)),
             ("ids must be torch", lambda: vc.embedding_fwd(ids.short(), table)),
             ("table has shape", lambda: vc.embedding_fwd(ids, table[0])),
