@@ -22,7 +22,9 @@ constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kOneBlock = 8192;   // most tokens that one workgroup sorts
 constexpr int kFillRows = 64;      // rows of the table that a workgroup looks through for zeros
 // Bytes of zeros beside the sort of one workgroup, or beside a pass of several, and most workgroups that write them. 65,536 tokens, 50,000 x
-// 1,536 in fp32, two passes, bf16 rows: 65 MB a pass 245 us in all, 98 MB 233, 131 MB 227, 154 MB (the whole table) 231; none 285.
+// 1,536 in fp32, two passes, bf16 rows, ids as words come (15,644 of them met): 65 MB a pass 245 us in all with the lookup, 98 MB 233, 131 MB 227,
+// 154 MB (the whole table) 231; none 285. Where nearly every row is met, what was written beside the sort is written twice: 131 MB a pass cost
+// 50 us of 208 there.
 constexpr int64_t kFillOne = (int64_t)128 << 20, kFillPass = (int64_t)128 << 20;
 constexpr int kFillGroups = 512;
 
@@ -274,7 +276,7 @@ __device__ __forceinline__ int64_t lower(const uint32_t* keys, int64_t lo, int64
   return lo;
 }
 
-template <class G, int N, int V>
+template <class G, int N, int V, bool ODD = true>
 __device__ __forceinline__ void write_row(const EmbeddingArgs& a, int64_t id, const Span<N>* s, float* sum) {
   G* g = (G*)a.grad + id * a.cols;
 #pragma unroll
@@ -283,13 +285,17 @@ __device__ __forceinline__ void write_row(const EmbeddingArgs& a, int64_t id, co
     for (int e = 0; e < N; ++e) sum[N * v + e] *= a.scale;
     if (a.add) {
       Cols<G, N> old;
-      load_cols(old, (const G*)g, s[v]);
+      load_cols<ODD>(old, (const G*)g, s[v]);
 #pragma unroll
       for (int e = 0; e < N; ++e) sum[N * v + e] += old[e];
     }
-    store_cols(g, sum + N * v, s[v]);
+    store_cols<ODD>(g, sum + N * v, s[v]);
   }
 }
+
+// Waits for all loads at once. Loads and stores are counted by one counter, and whether a row is written between two tokens only the
+// keys say: left to itself, the compiler waits for everything, the stores' round trips too, before each next token.
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0), the other counters as they are
 
 // Zeros to those of the rows [v0, v0 + kFillRows) before `filled` that no token met.
 template <class G>
@@ -314,10 +320,11 @@ __device__ __forceinline__ void fill_unmet(const EmbeddingArgs& a, int64_t v0) {
 
 // The first `sums` workgroups sum shares of the sorted tokens, the others write zeros. `across` threads a share; WHOLE: these are whole
 // waves, whose keys and positions lie in their lanes, 64 at a time, so that every row's address is a scalar and 16 rows are in
-// flight behind one load of positions.
-template <class D, class G, bool WHOLE>
+// flight behind one load of positions. ODD: rows may end within a vector. (The code that writes a row stands behind each of the rows in
+// flight, and with that of odd ends it is more than the instruction cache holds.)
+template <class D, class G, bool WHOLE, bool ODD>
 __global__ __launch_bounds__(1024) void embedding_sum_kernel(EmbeddingArgs a, int sums, int across) {
-  constexpr int N = Form<D, G>::N, V = Form<D, G>::V, U = WHOLE && sizeof(D) == 2 ? 16 : 8;  // U: rows of a thread in flight
+  constexpr int N = Form<D, G>::N, V = Form<D, G>::V, U = WHOLE && !ODD && sizeof(D) == 2 ? 16 : 8;  // U: rows of a thread in flight
   if ((int)blockIdx.x >= sums) return fill_unmet<G>(a, ((int64_t)blockIdx.x - sums) * kFillRows);
   const uint32_t *keys = a.keys[0], *pos = a.pos[0];
   const uint32_t none = (uint32_t)a.vocab;
@@ -336,9 +343,9 @@ __global__ __launch_bounds__(1024) void embedding_sum_kernel(EmbeddingArgs a, in
     if (cur >= none) return;
     if (from || on) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) store_cols(from ? part : part + a.cols, sum + N * v, s[v]);
+      for (int v = 0; v < V; ++v) store_cols<ODD>(from ? part : part + a.cols, sum + N * v, s[v]);
     } else {
-      write_row<G, N, V>(a, cur, s, sum);
+      write_row<G, N, V, ODD>(a, cur, s, sum);
     }
   };
   auto add = [&](uint32_t k, const Cols<D, N>* r) {
@@ -368,8 +375,9 @@ __global__ __launch_bounds__(1024) void embedding_sum_kernel(EmbeddingArgs a, in
         for (int u = 0; u < U; ++u) {
           const uint32_t p = __builtin_amdgcn_readlane(ps, min(u0 + u, real - 1));
 #pragma unroll
-          for (int v = 0; v < V; ++v) load_cols(r[u][v], (const D*)a.dout + (int64_t)p * a.dout_stride, s[v]);
+          for (int v = 0; v < V; ++v) load_cols<false>(r[u][v], (const D*)a.dout + (int64_t)p * a.dout_stride, s[v]);
         }
+        wait_loads();
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           if (u0 + u >= real) break;
@@ -395,6 +403,7 @@ __global__ __launch_bounds__(1024) void embedding_sum_kernel(EmbeddingArgs a, in
           if (k[u] < none) load_cols(r[u][v], (const D*)a.dout + (int64_t)pos[at] * a.dout_stride, s[v]);
         }
       }
+      wait_loads();
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (i + u >= i1) break;
@@ -544,10 +553,15 @@ hipError_t launch_embedding_bwd(EmbeddingArgs a, hipStream_t s) {
   const int sums = (p.chunks + shares - 1) / shares;
   const int fill = a.add ? 0 : (int)((a.filled + kFillRows - 1) / kFillRows);
   pick(a.out_f32, a.grad_f32, [&](auto d, auto g) {
-    if (least > 32)
-      hipLaunchKernelGGL((embedding_sum_kernel<decltype(d), decltype(g), true>), dim3(sums + fill), dim3(threads), 0, s, a, sums, across);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(sums + fill), dim3(threads), 0, s, a, sums, across); };
+    using D = decltype(d);
+    using G = decltype(g);
+    if (least <= 32)
+      launch(embedding_sum_kernel<D, G, false, true>);
+    else if (a.cols % Form<D, G>::N)
+      launch(embedding_sum_kernel<D, G, true, true>);
     else
-      hipLaunchKernelGGL((embedding_sum_kernel<decltype(d), decltype(g), false>), dim3(sums + fill), dim3(threads), 0, s, a, sums, across);
+      launch(embedding_sum_kernel<D, G, true, false>);
   });
   if (p.chunks > 1) {
     const dim3 grid(p.chunks, (a.cols + 255) / 256), block(kJoinThreads, kJoinRuns);

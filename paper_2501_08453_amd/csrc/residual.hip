@@ -641,7 +641,8 @@ void residual_groups(int64_t rows, int cols, bool backward, int* groups, int* ch
   const int threads = backward ? bwd_across(cols) : threads_of(cols), abreast = backward ? bwd_abreast(cols) : 1;
   const int waves = !backward ? kFwdWaves : cols <= kFewCols ? kBwdWaves : 2;
   const int64_t most = 256 * std::max(1, 4 * waves / (threads / 64 * abreast));  // as many as 256 compute units hold
-  const int64_t c = ((rows + most - 1) / most + abreast - 1) / abreast * abreast;
+  // a run of the backward has four rows at least, or its sums weigh more than they: 780 x 3,568 28.7 us so, 34.9 with one, 29.9 with eight
+  const int64_t c = (std::max<int64_t>((rows + most - 1) / most, backward ? 4 : 1) + abreast - 1) / abreast * abreast;
   *chunk = (int)c;
   *groups = (int)((rows + c - 1) / c);
 }
