@@ -587,7 +587,7 @@ vc_status vc_residualnorm_fwd(const vc_residualnorm_desc* desc,
 /* Bytes of device workspace of the backward (runs' and samples' column sums); 0 for an invalid descriptor. Host only. */
 size_t vc_residualnorm_bwd_workspace_bytes(const vc_residualnorm_desc* desc);
 
-/* h and a: as the forward had them (h written by it, a contiguous or a_stride apart), or its h8 and a8 with their scales.
+/* h and a: as the forward had them (h written by it, or without a the x, x_stride apart), or its h8 and a8 with their scales.
  * dh or dy may be NULL (0), every output too (not wanted); without the vectors' gradients the workspace may be NULL. */
 vc_status vc_residualnorm_bwd(const vc_residualnorm_desc* desc,
                               const void* dh, const void* dy, const void* h, const void* a,
@@ -602,7 +602,7 @@ vc_status vc_residualnorm_bwd(const vc_residualnorm_desc* desc,
  * Activation checkpoints in 8 bits (Sec. V-B trades activation memory against time; this keeps
  * an activation at half of its 16 bits). Each block of 128 columns of a row (the last one may be shorter), with
  * m = max(the largest |x| of the block, 2^-100):
- *   scale = m / 127, q = x * (127 / m) rounded to the nearest whole number (ties to even), -127 .. 127, x' = q * scale,
+ *   scale = m / 127 (at most the largest number whose 127 fold is finite), q = x * (127 / m) rounded to the nearest whole number (ties to even), -127 .. 127, x' = q * scale,
  * in fp32: off by at most half a step, m / 254, and that rounding. A block that holds an infinity or a NaN has a scale of NaN, and
  * unpacks to NaN. q: int8 [rows, cols], scales: fp32 [rows, ceil(cols / 128)], both contiguous.
  * ------------------------------------------------------------------------- */

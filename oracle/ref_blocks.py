@@ -7,6 +7,8 @@ from __future__ import annotations
 
 import numpy as np
 
+TOP_SCALE = np.float32(float.fromhex("0x1.020406p+121"))  # the largest whose 127 fold is finite in fp32
+
 
 def normed(t, kind, eps):
     """(normed t, mean, reciprocal deviation) over the last axis."""
@@ -69,7 +71,7 @@ def kept8(x):
             part = x[:, 128 * b:128 * b + 128]
             good = np.isfinite(part).all(1)
             m = np.where(good, np.maximum(np.abs(np.where(np.isfinite(part), part, 0)).max(1), f(2.0 ** -100)), f(1)).astype(f)
-            scale = np.where(good, m / f(127), f(np.nan)).astype(f)
+            scale = np.where(good, np.minimum(m / f(127), TOP_SCALE), f(np.nan)).astype(f)
             w = np.where(good[:, None], np.rint(part * (f(127) / m)[:, None]), f(0)).astype(f)
             q[:, 128 * b:128 * b + 128] = w.astype(np.int64)
             scales[:, b] = scale

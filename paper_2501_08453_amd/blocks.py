@@ -111,8 +111,8 @@ def _call_on(device, name, desc, *args):
     more time here than on the GPU, hence no wrapper for each argument."""
     import torch
     if not _CURRENT:
-        _CURRENT.append(getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device))
-        _CURRENT.append(getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream))
+        _CURRENT[:] = (getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),  # both at once: threads share it
+                       getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream))
     number, stream = _CURRENT
     f = getattr(_lib(), name)
     p = [t if t is None or type(t) is int else t.data_ptr() for t in args]
@@ -127,6 +127,7 @@ def _call_on(device, name, desc, *args):
 
 
 _TYPES = {}
+_COLS = 0x7fffffff  # more columns than any descriptor takes: what a call with more of them says, not the number's low 32 bits
 
 
 def _type(name, t):
@@ -153,6 +154,21 @@ def _vector(name, p, cols, S, every, dtype):
     return p.stride(0)
 
 
+def _vectors(d, every, gate, scale, shift, post_weight):
+    """Appends the parameters of a call to its checks, and sets the descriptor's type and strides of them."""
+    cols, dtype = d.cols, None
+    for name, p in (("gate", gate), ("scale", scale), ("shift", shift), ("post_weight", post_weight)):
+        if p is None:
+            continue
+        if dtype is None:
+            dtype = p.dtype
+            d.param_type = _type("gate, scale, shift and post_weight", p)
+        if name == "post_weight":
+            every.append((name, p, (cols,), dtype, False))
+        else:
+            setattr(d, name + "_stride", _vector(name, p, cols, d.samples, every, dtype))
+
+
 def _residual_desc(desc, x, a, gate, scale, shift, post_weight, cu, lens, y_type):
     """A copy of the descriptor with the types and strides of the tensors of one call, checked."""
     import torch
@@ -166,19 +182,7 @@ def _residual_desc(desc, x, a, gate, scale, shift, post_weight, cu, lens, y_type
     if a is not None:
         every.append(("a", a, shape, a.dtype, True))
         d.a_stride = _row_stride("a", a)
-    dtype = None
-    for name, p in (("gate", gate), ("scale", scale), ("shift", shift), ("post_weight", post_weight)):
-        if p is None:
-            continue
-        if dtype is None:
-            dtype = p.dtype
-            d.param_type = _type("gate, scale, shift and post_weight", p)
-        if name == "post_weight":
-            every.append((name, p, (cols,), dtype, False))
-        else:
-            stride = _vector(name, p, cols, S, every, dtype)
-            if stride:
-                setattr(d, name + "_stride", stride)
+    _vectors(d, every, gate, scale, shift, post_weight)
     if cu is not None:
         d.packed = 1
         every.append(("cu", cu, (S + 1,), torch.int32, False))
@@ -265,8 +269,26 @@ def residual_norm_bwd(dh, dy, saved, ws=None, want=(True,) * 6):
         d.dy_stride = _row_stride("dy", dy)
     if s.stats is not None:
         every.append(("saved.stats", s.stats, (4, d.rows), torch.float32, False))
-    else:
-        every.append(("saved.a", a, shape, a.dtype, True))
+    # What was saved may lie otherwise than it did (a hook of the saved tensors packs strided ones close, say).
+    blocks = (d.rows, (d.cols + BLOCK - 1) // BLOCK)
+    for name, t, scales, of in (("h", h, hs, d.x_type), ("a", a, as_, d.y_type)):
+        if t is None:
+            continue
+        every.append(("saved." + name, t, shape, torch.int8 if d.checkpoint else types[of], not d.checkpoint))
+        if d.checkpoint:
+            every.append(("saved.%s.scales" % name, scales, blocks, torch.float32, False))
+    if not d.checkpoint:
+        if a is not None:
+            d.a_stride = _row_stride("saved.a", a)
+        elif h is not None:
+            d.x_stride = _row_stride("saved.h", h)
+        if a is not None and h is not None and not h.is_contiguous():
+            raise ValueError("saved.h must be contiguous")
+    _vectors(d, every, s.gate, s.scale, s.shift, s.post_weight)
+    if s.cu is not None:
+        every.append(("saved.cu", s.cu, (d.samples + 1,), torch.int32, False))
+    if s.lens is not None:
+        every.append(("saved.lens", s.lens, (d.samples,), torch.int32, False))
     _check_all(every)
     dev = every[0][1].device
     dx = torch.empty(shape, dtype=types[d.x_type], device=dev) if want[0] else None
@@ -317,7 +339,7 @@ def checkpoint_pack(x, out=None):
         _check_all([("x", x, x.shape, x.dtype, True), ("out.q", out.q, x.shape, torch.int8, False),
                     ("out.scales", out.scales, blocks, torch.float32, False)])
     if rows:
-        _call_on(x.device, "vc_checkpoint_pack", vc_checkpoint_desc(rows, cols, f32, stride), x, kept.q, kept.scales)
+        _call_on(x.device, "vc_checkpoint_pack", vc_checkpoint_desc(rows, min(cols, _COLS), f32, stride), x, kept.q, kept.scales)
     return kept
 
 
@@ -335,20 +357,20 @@ def checkpoint_unpack(kept, dtype=None, out=None):
                 ("scales", scales, q.shape[:-1] + ((cols + BLOCK - 1) // BLOCK,), torch.float32, False),
                 ("out", out, q.shape, out.dtype, False)])
     if rows:
-        _call_on(q.device, "vc_checkpoint_unpack", vc_checkpoint_desc(rows, cols, f32, 0), q, scales, out)
+        _call_on(q.device, "vc_checkpoint_unpack", vc_checkpoint_desc(rows, min(cols, _COLS), f32, 0), q, scales, out)
     return out
 
 
 def saved_in_8bit(min_elements=1 << 16):
-    """A context in which autograd keeps activations in 8 bits: tensors of bf16, of at least min_elements elements, two
+    """A context in which autograd keeps activations in 8 bits: contiguous tensors of bf16, of at least min_elements elements, two
     dimensions and 64 columns, that an operation saves for its backward are packed, and unpacked where the backward asks for
-    them. Leaves (parameters, inputs) stay as they are, for they are kept anyway, and so do tensors of 32 bits (log-sum-exps,
-    statistics). An attention's backward then computes its probabilities from the kept q and k."""
+    them. Leaves (parameters, inputs) and views of them stay as they are, for they are kept anyway, and so do tensors of 32 bits
+    (log-sum-exps, statistics). A tensor that several operations save is packed for each of them. An attention's backward then computes its probabilities from the kept q and k."""
     import torch
 
     def pack(t):
         if (t.device.type != "cuda" or t.dtype is not torch.bfloat16 or t.dim() < 2 or
-                t.numel() < min_elements or t.is_leaf or t.shape[-1] < 64 or not t.is_contiguous()):
+                t.numel() < min_elements or (t if t._base is None else t._base).is_leaf or t.shape[-1] < 64 or not t.is_contiguous()):
             return t
         return checkpoint_pack(t.detach())
 
@@ -384,7 +406,7 @@ def embedding_fwd(ids, table, scale=1.0, padding_id=None, dtype=None, out=None):
     of = _type("out", out)
     _check_all([("ids", ids, ids.shape, ids.dtype, False), ("table", table, (V, cols), table.dtype, True),
                 ("out", out, ids.shape + (cols,), out.dtype, False)])
-    desc = vc_embedding_desc(ids.numel(), V, -1 if padding_id is None else padding_id, _row_stride("table", table), cols, i64, tf,
+    desc = vc_embedding_desc(ids.numel(), V, -1 if padding_id is None else padding_id, _row_stride("table", table), min(cols, _COLS), i64, tf,
                              of, scale, 0)
     if desc.tokens:
         _call_on(table.device, "vc_embedding_fwd", desc, ids, table, out)
@@ -407,7 +429,7 @@ def embedding_bwd(dout, ids, vocab, scale=1.0, padding_id=None, dtype=None, into
     gf = _type("dtable", grad)
     _check_all([("dout", dout, ids.shape + (cols,), dout.dtype, True), ("ids", ids, ids.shape, ids.dtype, False),
                 ("into", grad, (vocab, cols), grad.dtype, False)])
-    desc = vc_embedding_desc(ids.numel(), vocab, -1 if padding_id is None else padding_id, _row_stride("dout", dout), cols, i64,
+    desc = vc_embedding_desc(ids.numel(), vocab, -1 if padding_id is None else padding_id, _row_stride("dout", dout), min(cols, _COLS), i64,
                              gf, of, scale, 0 if into is None else 1)
     if not desc.tokens:
         return grad.zero_() if into is None else grad

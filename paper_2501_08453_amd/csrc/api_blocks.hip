@@ -188,6 +188,7 @@ vc_status vc_residualnorm_bwd(const vc_residualnorm_desc* desc, const void* dh, 
     r.a8s = const_cast<float*>(a8_scales);
   } else {
     r.h_in = h;
+    r.h_stride = a ? desc->cols : r.x_stride;  // without a block output h is x itself
     r.a = a;
   }
   r.gate = gate;

@@ -324,7 +324,7 @@ void residual_bwd_kernel(ResidualArgs a, int across) {
   const int r1 = min(a.rows, ((int)blockIdx.x + 1) * a.chunk), blocks = (C + kBlockOf8 - 1) / kBlockOf8;
   const HT* hp = K8 ? (const HT*)a.h8 : (const HT*)a.h_in;
   const AT* ap = K8 ? (const AT*)a.a8 : (const AT*)a.a;
-  const int64_t a_stride = K8 ? C : a.a_stride;
+  const int64_t h_stride = K8 ? C : a.h_stride, a_stride = K8 ? C : a.a_stride;
   const bool has_a = ap != nullptr, has_norm = a.norm != VC_NORM_NONE && a.dy;
   float sa[W] = {}, se[W] = {}, sf[W] = {};
   // This run's sums to the row `to` of the partials: those of the rows abreast added in order.
@@ -377,7 +377,7 @@ void residual_bwd_kernel(ResidualArgs a, int across) {
         if (a.dh) load_cols<ODD, ONCE>(dh[v], (const X*)a.dh + row * a.dh_stride, sp[v]);
         if (has_norm) {
           load_cols<ODD, ONCE>(dy[v], (const Y*)a.dy + row * a.dy_stride, sp[v]);
-          load_cols<ODD, ONCE>(h[v], hp + row * C, sp[v]);
+          load_cols<ODD, ONCE>(h[v], hp + row * h_stride, sp[v]);
           if (K8) hs[v] = a.h8s[row * blocks + block[v]];
         }
         if (has_a) {

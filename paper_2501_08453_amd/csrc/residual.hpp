@@ -23,7 +23,7 @@ struct ResidualArgs {
   float* part;                                // [groups + samples][3][cols]: each run's sums of H xa, dy xh, dy
   float* sums;                                // [samples][3][cols], where sums over samples are wanted
   const int32_t *cu, *lens;
-  int64_t x_stride, a_stride, dh_stride, dy_stride;
+  int64_t x_stride, a_stride, dh_stride, dy_stride, h_stride;  // h_stride: of h_in
   int64_t gate_stride, scale_stride, shift_stride;  // elements between samples; 0: one for all of them
   int rows, cols, samples, per;               // per: rows of a sample's slot (without cu)
   int groups, chunk;                          // workgroups, and the rows of each

@@ -19,6 +19,7 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kBlockOf8 = 128;  // columns of a row that share a checkpoint's scale
+constexpr float kTopScale = 0x1.020406p+121f;
 
 // A vector as it lies in memory, at any multiple of its elements' size: rows of odd length, or of odd stride, start anywhere (the
 // hardware takes such addresses in its wide loads and stores of global memory).
@@ -206,6 +207,7 @@ __device__ __forceinline__ float wave_sum(float x) {
 // The 8-bit form of a block of 128 columns, N in each of 128 / N lanes (zeros where they are not a lane's own): whole steps of
 // a 127th of the largest magnitude, at least 2^-100. The largest is found over the bits of |x|, where a NaN is larger than an
 // infinity and that than any number: such a block's scale is NaN, and so is all that is unpacked from it.
+// Scales are at most the largest number whose 127 fold is finite: that of the largest fp32 numbers is a step of 2^-24 below theirs.
 // |x (127 / top)| is at most 127 (1 + 2^-23), which rounds to 127.
 template <int N>
 struct Kept {
@@ -226,7 +228,7 @@ __device__ __forceinline__ Kept<N> keep(const float* x) {
   const float m = finite ? fmaxf(__uint_as_float(top), 0x1p-100f) : 1.0f;
   const float inv = 127.0f / m;
   Kept<N> k;
-  k.scale = finite ? m / 127.0f : __uint_as_float(0x7fc00000u);
+  k.scale = finite ? fminf(m / 127.0f, kTopScale) : __uint_as_float(0x7fc00000u);
   uint32_t w[N / 4];
 #pragma unroll
   for (int i = 0; i < N / 4; ++i) {

@@ -87,3 +87,11 @@ def test_embedding_and_gradient():
     # <dout, d out> = <gradient, d table>
     d = g.standard_normal((7, 3))
     assert np.isclose((dout * B.embedding(ids, d, 0.5, 0)).sum(), (grad * d).sum()) and (mag >= np.abs(grad) - 1e-12).all()
+
+
+def test_top_scale_is_the_largest_of_a_finite_127_fold():
+    f = np.float32
+    with np.errstate(over="ignore"):
+        assert np.isfinite(f(127) * B.TOP_SCALE) and np.isinf(f(127) * np.nextafter(B.TOP_SCALE, f(np.inf)))
+    vals, _, _ = B.kept8(np.array([[np.finfo(f).max, 1.0, -np.finfo(f).max]], f))
+    assert np.isfinite(vals).all()
