@@ -28,10 +28,20 @@ constexpr int kFillRows = 64;      // rows of the table that a workgroup looks t
 constexpr int64_t kFillOne = (int64_t)128 << 20, kFillPass = (int64_t)128 << 20;
 constexpr int kFillGroups = 512;
 
-// The id of token t; `vocab`, which is none, where it is the padding's or none of the table's.
-__device__ __forceinline__ int64_t id_of(const EmbeddingArgs& a, int64_t t) {
-  const int64_t id = a.ids64 ? ((const int64_t*)a.ids)[t] : (int64_t)((const int32_t*)a.ids)[t];
-  return id < 0 || id >= a.vocab || id == a.padding ? a.vocab : id;
+// The ids of K tokens at(0), at(1), ..., all in flight at once (so no branch stands between two of them, and every place exists);
+// `vocab`, which is none, where it is the padding's or none of the table's.
+template <int K, class At>
+__device__ __forceinline__ void ids_of(const EmbeddingArgs& a, uint32_t* key, At at) {
+  int64_t id[K];
+  if (a.ids64) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) id[k] = ((const int64_t*)a.ids)[at(k)];
+  } else {
+#pragma unroll
+    for (int k = 0; k < K; ++k) id[k] = ((const int32_t*)a.ids)[at(k)];
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) key[k] = (uint32_t)(id[k] < 0 || id[k] >= a.vocab || id[k] == a.padding ? a.vocab : id[k]);
 }
 
 // A row of threads: `across` of them, V vectors of N columns each.
@@ -55,13 +65,14 @@ __global__ __launch_bounds__(1024) void embedding_fwd_kernel(EmbeddingArgs a) {
   const int64_t step = (int64_t)gridDim.x * rows;
   for (int64_t t = (int64_t)blockIdx.x * rows + ty; t < a.tokens; t += U * step) {
     Cols<T, N> r[U][V];
+    uint32_t id[U];
+    ids_of<U>(a, id, [&](int u) { return min(t + u * step, a.tokens - 1); });
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t id = t + u * step < a.tokens ? id_of(a, t + u * step) : a.vocab;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         r[u][v] = Cols<T, N>{};
-        if (id < a.vocab) load_cols(r[u][v], (const T*)a.table + id * a.table_stride, s[v]);
+        if (id[u] < (uint32_t)a.vocab && t + u * step < a.tokens) load_cols(r[u][v], (const T*)a.table + id[u] * a.table_stride, s[v]);
       }
     }
 #pragma unroll
@@ -100,22 +111,50 @@ __device__ __forceinline__ void fill_rows(const EmbeddingArgs& a, int64_t v0, in
 // Ranks of this wave's ITEMS x 64 digits (item k of lane l is number 64 k + l) among those before with the same digit;
 // count: the wave's own counters, zeros before.
 template <int ITEMS>
-__device__ __forceinline__ void wave_ranks(const uint32_t* digit, const bool* real, uint32_t* rank, uint32_t* count) {
+__device__ __forceinline__ void wave_ranks(const uint32_t* digit, const bool* real, uint32_t* rank, uint32_t* count, int bits) {
   const int lane = threadIdx.x & 63;
+  uint32_t lo[ITEMS], hi[ITEMS], base[ITEMS];  // the lanes of the same digit
+  int first[ITEMS];
 #pragma unroll
   for (int k = 0; k < ITEMS; ++k) {
-    uint64_t same = __ballot(real[k]);
+    const uint64_t m = __ballot(real[k]);
+    lo[k] = (uint32_t)m;
+    hi[k] = (uint32_t)(m >> 32);
+  }
+  for (int b = 0; b < bits; ++b)
 #pragma unroll
-    for (int b = 0; b < kDigitBits; ++b) {
-      const bool one = digit[k] >> b & 1;
-      const uint64_t m = __ballot(one);
-      same &= one ? m : ~m;
+    for (int k = 0; k < ITEMS; ++k) {
+      const uint32_t one = (uint32_t)__builtin_amdgcn_sbfe((int)digit[k], b, 1);  // all of its bits
+      const uint64_t m = __ballot(one != 0);
+      lo[k] &= ~((uint32_t)m ^ one);
+      hi[k] &= ~((uint32_t)(m >> 32) ^ one);
     }
-    const int first = real[k] ? __ffsll((unsigned long long)same) - 1 : lane;
-    uint32_t base = 0;
-    if (real[k] && lane == first) base = atomicAdd(&count[digit[k]], (uint32_t)__popcll(same));
-    base = __shfl(base, first, 64);
-    rank[k] = base + __popcll(same & (((uint64_t)1 << lane) - 1));
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k) {
+    first[k] = !real[k] ? lane : lo[k] ? __ffs((int)lo[k]) - 1 : __ffs((int)hi[k]) + 31;
+    base[k] = 0;
+    if (real[k] && lane == first[k]) base[k] = atomicAdd(&count[digit[k]], (uint32_t)(__popc(lo[k]) + __popc(hi[k])));
+  }
+#pragma unroll
+  for (int k = 0; k < ITEMS; ++k)
+    rank[k] = __shfl(base[k], first[k], 64) + __builtin_amdgcn_mbcnt_hi(hi[k], __builtin_amdgcn_mbcnt_lo(lo[k], 0));
+}
+
+// The waves' counts of each digit to where their tokens of it begin: behind `before`, the wave before and all smaller digits.
+// total: of the digit, in all waves. For the first 512 threads, one a digit.
+__device__ __forceinline__ uint32_t waves_total(const uint32_t (*count)[kDigits], uint32_t* c) {
+  uint32_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) c[w] = count[w][threadIdx.x];
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) total += c[w];
+  return total;
+}
+__device__ __forceinline__ void waves_begin(uint32_t (*count)[kDigits], const uint32_t* c, uint32_t before) {
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) {
+    count[w][threadIdx.x] = before;
+    before += c[w];
   }
 }
 
@@ -143,31 +182,25 @@ __global__ __launch_bounds__(kSortThreads) void embedding_sort_one_kernel(Embedd
   __shared__ uint32_t tmp[8];
   const int t = threadIdx.x, wave = t >> 6, lane = t & 63, T = (int)a.tokens;
   const int at = wave * 64 * ITEMS + lane;
+  const int digits = 1 << a.digits;
   uint32_t key[ITEMS], p[ITEMS], rank[ITEMS], digit[ITEMS];
   bool real[ITEMS];
 #pragma unroll
   for (int k = 0; k < ITEMS; ++k) {
     p[k] = at + 64 * k;
     real[k] = (int)p[k] < T;
-    key[k] = real[k] ? (uint32_t)id_of(a, p[k]) : 0;
   }
+  ids_of<ITEMS>(a, key, [&](int k) { return min((int)p[k], T - 1); });
   for (int pass = 0; pass < a.passes; ++pass) {
-    for (int i = lane; i < kDigits; i += 64) count[wave][i] = 0;
+    for (int i = lane; i < digits; i += 64) count[wave][i] = 0;
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k) digit[k] = key[k] >> (pass * a.digits) & ((1u << a.digits) - 1);
     __syncthreads();
-    wave_ranks<ITEMS>(digit, real, rank, count[wave]);
+    wave_ranks<ITEMS>(digit, real, rank, count[wave], a.digits);
     __syncthreads();
-    uint32_t all = 0;
-    if (t < kDigits)
-      for (int w = 0; w < kSortWaves; ++w) {
-        const uint32_t c = count[w][t];
-        count[w][t] = all;
-        all += c;
-      }
-    const uint32_t before = scan512(t < kDigits ? all : 0, tmp);
-    if (t < kDigits)
-      for (int w = 0; w < kSortWaves; ++w) count[w][t] += before;
+    uint32_t c[kSortWaves];
+    const uint32_t before = scan512(t < digits ? waves_total(count, c) : 0, tmp);
+    if (t < digits) waves_begin(count, c, before);
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < ITEMS; ++k)
@@ -192,8 +225,12 @@ __global__ __launch_bounds__(kSortThreads) void embedding_sort_one_kernel(Embedd
     }
 }
 
-__device__ __forceinline__ uint32_t sort_key(const EmbeddingArgs& a, int pass, int64_t i) {
-  return pass == 0 ? (uint32_t)id_of(a, i) : a.keys[pass & 1][i];
+// The keys of K tokens at a pass, at places that exist.
+template <int K, class At>
+__device__ __forceinline__ void sort_keys(const EmbeddingArgs& a, int pass, uint32_t* key, At at) {
+  if (pass == 0) return ids_of<K>(a, key, at);
+#pragma unroll
+  for (int k = 0; k < K; ++k) key[k] = a.keys[pass & 1][at(k)];
 }
 
 // Several workgroups: how often each digit stands in each block's tokens.
@@ -204,11 +241,12 @@ __global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(Embedding
   const int t = threadIdx.x;
   if (t < kDigits) count[t] = 0;
   __syncthreads();
+  const int64_t at = (int64_t)blockIdx.x * kSortThreads * ITEMS + t;
+  uint32_t key[ITEMS];
+  sort_keys<ITEMS>(a, pass, key, [&](int k) { return min(at + k * kSortThreads, a.tokens - 1); });
 #pragma unroll
-  for (int k = 0; k < ITEMS; ++k) {
-    const int64_t i = (int64_t)blockIdx.x * kSortThreads * ITEMS + k * kSortThreads + t;
-    if (i < a.tokens) atomicAdd(&count[sort_key(a, pass, i) >> (pass * a.digits) & ((1u << a.digits) - 1)], 1u);
-  }
+  for (int k = 0; k < ITEMS; ++k)
+    if (at + k * kSortThreads < a.tokens) atomicAdd(&count[key[k] >> (pass * a.digits) & ((1u << a.digits) - 1)], 1u);
   __syncthreads();
   if (t < kDigits) a.hist[(int64_t)blockIdx.x * kDigits + t] = count[t];
 }
@@ -224,16 +262,22 @@ __global__ __launch_bounds__(kSortThreads) void embedding_move_kernel(EmbeddingA
   uint32_t key[ITEMS], p[ITEMS], rank[ITEMS], digit[ITEMS];
   bool real[ITEMS];
   for (int i = lane; i < kDigits; i += 64) count[wave][i] = 0;
+  auto place = [&](int k) { return min(at + 64 * k, a.tokens - 1); };
+  sort_keys<ITEMS>(a, pass, key, place);
+  if (pass) {
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) p[k] = a.pos[pass & 1][place(k)];
+  } else {
+#pragma unroll
+    for (int k = 0; k < ITEMS; ++k) p[k] = (uint32_t)place(k);
+  }
 #pragma unroll
   for (int k = 0; k < ITEMS; ++k) {
-    const int64_t i = at + 64 * k;
-    real[k] = i < a.tokens;
-    key[k] = real[k] ? sort_key(a, pass, i) : 0;
-    p[k] = !real[k] ? 0 : pass == 0 ? (uint32_t)i : a.pos[pass & 1][i];
+    real[k] = at + 64 * k < a.tokens;
     digit[k] = key[k] >> (pass * a.digits) & ((1u << a.digits) - 1);
   }
   __syncthreads();
-  wave_ranks<ITEMS>(digit, real, rank, count[wave]);
+  wave_ranks<ITEMS>(digit, real, rank, count[wave], a.digits);
   __syncthreads();
   uint32_t total = 0, mine = 0;  // of this digit: in all blocks, in those before
   if (t < kDigits)
@@ -245,12 +289,9 @@ __global__ __launch_bounds__(kSortThreads) void embedding_move_kernel(EmbeddingA
     }
   const uint32_t before = scan512(t < kDigits ? total : 0, tmp) + mine;
   if (t < kDigits) {
-    uint32_t all = before;
-    for (int w = 0; w < kSortWaves; ++w) {
-      const uint32_t c = count[w][t];
-      count[w][t] = all;
-      all += c;
-    }
+    uint32_t c[kSortWaves];
+    waves_total(count, c);
+    waves_begin(count, c, before);
   }
   __syncthreads();
 #pragma unroll
@@ -423,15 +464,18 @@ __global__ __launch_bounds__(kJoinThreads * kJoinRuns) void embedding_join_kerne
   const uint32_t* keys = a.keys[0];
   const int64_t T = a.tokens, c = blockIdx.x, i0 = c * a.chunk, i1 = i0 + a.chunk;
   if (i1 >= T) return;
-  const uint32_t id = keys[i1 - 1], next = keys[i1], begin = keys[i0], before = keys[max(i0 - 1, (int64_t)0)];
-  if (id >= (uint32_t)a.vocab || next != id || (begin == id && i0 > 0 && before == id)) return;
   const int t = threadIdx.x, y = threadIdx.y, lane = (y * kJoinThreads + t) & 63;
+  const int64_t behind = i1 + (int64_t)lane * a.chunk;
+  const uint32_t id = keys[i1 - 1], next = keys[i1], begin = keys[i0], before = keys[max(i0 - 1, (int64_t)0)];
+  uint32_t first = keys[min(behind, T - 1)];
+  if (id >= (uint32_t)a.vocab || next != id || (begin == id && i0 > 0 && before == id)) return;
   int count = 1;  // shares of this id: those behind begin with it; 64 of them a step
-  for (bool more = true; more;) {
-    const int64_t at = (c + count + lane) * a.chunk;
-    const uint64_t other = ~__ballot(at < T && keys[min(at, T - 1)] == id);
-    more = !other;
+  for (int64_t at = behind;;) {
+    const uint64_t other = ~__ballot(at < T && first == id);
     count += other ? __ffsll((unsigned long long)other) - 1 : 64;
+    if (other) break;
+    at += (int64_t)64 * a.chunk;
+    first = keys[min(at, T - 1)];
   }
   Span<4> s[2];
 #pragma unroll
