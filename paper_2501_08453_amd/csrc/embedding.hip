@@ -55,7 +55,7 @@ __device__ __forceinline__ void spans_of(Span<N>* s, int t, int across, int C) {
   for (int v = 0; v < V; ++v) s[v] = span_at<N>((v * across + t) * N, C);
 }
 
-template <class T, class O>
+template <class T, class O, bool ONCE>
 __global__ __launch_bounds__(1024) void embedding_fwd_kernel(EmbeddingArgs a) {
   constexpr int U = 4, N = Form<T, O>::N, V = Form<T, O>::V;  // U: tokens of a thread in flight
   const int across = (a.cols + 7) / 8, rows = blockDim.x / across, ty = threadIdx.x / across;
@@ -83,24 +83,33 @@ __global__ __launch_bounds__(1024) void embedding_fwd_kernel(EmbeddingArgs a) {
         float x[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) x[e] = r[u][v][e] * a.scale;
-        store_cols((O*)a.out + (t + u * step) * a.cols, x, s[v]);
+        store_cols<true, ONCE>((O*)a.out + (t + u * step) * a.cols, x, s[v]);
       }
     }
   }
 }
 
 // Zeros to rows [v0, v1) of the gradient: by workgroup `at` of `of` that do so.
-__device__ __forceinline__ void fill_rows(const EmbeddingArgs& a, int64_t v0, int64_t v1, int at, int of) {
+template <bool ONCE>
+__device__ __forceinline__ void fill_rows_as(const EmbeddingArgs& a, int64_t v0, int64_t v1, int at, int of) {
   const int64_t n = (v1 - v0) * a.cols * (a.grad_f32 ? 4 : 2);  // bytes, whole elements
   char* p = (char*)a.grad + v0 * a.cols * (a.grad_f32 ? 4 : 2);
   typedef f32x4 any __attribute__((aligned(2)));
   const int64_t step = (int64_t)of * blockDim.x * 16;
   for (int64_t i = ((int64_t)at * blockDim.x + threadIdx.x) * 16; i < n; i += step) {
-    if (i + 16 <= n)
-      *(any*)(p + i) = f32x4{};
-    else
+    if (i + 16 > n)
       for (int64_t j = i; j < n; j += 2) *(uint16_t*)(p + j) = 0;
+    else if constexpr (ONCE)
+      __builtin_nontemporal_store(f32x4{}, (any*)(p + i));
+    else
+      *(any*)(p + i) = f32x4{};
   }
+}
+__device__ __forceinline__ void fill_rows(const EmbeddingArgs& a, int64_t v0, int64_t v1, int at, int of) {
+  if (a.once)
+    fill_rows_as<true>(a, v0, v1, at, of);
+  else
+    fill_rows_as<false>(a, v0, v1, at, of);
 }
 
 // --- sort ---------------------------------------------------------------------------------------
@@ -363,7 +372,7 @@ __device__ __forceinline__ void fill_unmet(const EmbeddingArgs& a, int64_t v0) {
 // waves, whose keys and positions lie in their lanes, 64 at a time, so that every row's address is a scalar and 16 rows are in
 // flight behind one load of positions. ODD: rows may end within a vector. (The code that writes a row stands behind each of the rows in
 // flight, and with that of odd ends it is more than the instruction cache holds.)
-template <class D, class G, bool WHOLE, bool ODD>
+template <class D, class G, bool WHOLE, bool ODD, bool ONCE>
 __global__ __launch_bounds__(1024) void embedding_sum_kernel(EmbeddingArgs a, int sums, int across) {
   constexpr int N = Form<D, G>::N, V = Form<D, G>::V, U = WHOLE && !ODD && sizeof(D) == 2 ? 16 : 8;  // U: rows of a thread in flight
   if ((int)blockIdx.x >= sums) return fill_unmet<G>(a, ((int64_t)blockIdx.x - sums) * kFillRows);
@@ -416,7 +425,7 @@ __global__ __launch_bounds__(1024) void embedding_sum_kernel(EmbeddingArgs a, in
         for (int u = 0; u < U; ++u) {
           const uint32_t p = __builtin_amdgcn_readlane(ps, min(u0 + u, real - 1));
 #pragma unroll
-          for (int v = 0; v < V; ++v) load_cols<false>(r[u][v], (const D*)a.dout + (int64_t)p * a.dout_stride, s[v]);
+          for (int v = 0; v < V; ++v) load_cols<false, ONCE>(r[u][v], (const D*)a.dout + (int64_t)p * a.dout_stride, s[v]);
         }
         wait_loads();
 #pragma unroll
@@ -520,6 +529,14 @@ void pick(bool first, bool second, F go) {
   else
     with(__bf16{});
 }
+// Whether a call's streams (a lookup's output; the zeros beside the sort and the rows of dout) go past the caches: where these are in the
+// way of what is used again, rows of the table or of the gradient. ids as words come, bf16 rows, us without and with, alternating
+// with the other direction and by themselves: 65,536 x 1,536 lookups (384 MiB read and written) 62 and 46, 32,768 (192) 26 and 25; gradients of
+// 65,536 tokens in 32,128 x 1,536 fp32 (380 MiB) 128 and 110, with the lookup 208 and 154; of 30,000 in 60,000 x 1,024 bf16 (176) 60 and 60, 87 and 74;
+// of 8,192 in 32,128 x 1,024 fp32 (142) 35 and 42, 44 and 50. Not where a thread's vector takes two instructions, half of a line each.
+constexpr int64_t kOnceFwd = (int64_t)256 << 20, kOnceBwd = (int64_t)160 << 20;
+template <class X, class Y>
+constexpr bool kWholeLines = sizeof(X) * Form<X, Y>::N <= 16;
 int items(int64_t tokens) { return tokens <= 131072 ? 4 : 16; }
 
 }  // namespace
@@ -541,8 +558,14 @@ EmbeddingPlan embedding_plan(int64_t tokens, int64_t vocab, int cols) {
 hipError_t launch_embedding_fwd(const EmbeddingArgs& a, hipStream_t s) {
   const int threads = row_threads(a.cols, kRowThreads), rows = threads / ((a.cols + 7) / 8);
   const int64_t blocks = std::min<int64_t>(4096, (a.tokens + rows - 1) / rows);
+  const bool once = a.tokens * a.cols * ((a.table_f32 ? 4 : 2) + (a.out_f32 ? 4 : 2)) > kOnceFwd;
   pick(a.table_f32, a.out_f32, [&](auto t, auto o) {
-    hipLaunchKernelGGL((embedding_fwd_kernel<decltype(t), decltype(o)>), dim3(blocks), dim3(threads), 0, s, a);
+    using T = decltype(t);
+    using O = decltype(o);
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(threads), 0, s, a); };
+    if constexpr (kWholeLines<O, T>)
+      if (once) return launch(embedding_fwd_kernel<T, O, true>);
+    launch(embedding_fwd_kernel<T, O, false>);
   });
   return hipGetLastError();
 }
@@ -553,6 +576,7 @@ hipError_t launch_embedding_bwd(EmbeddingArgs a, hipStream_t s) {
   a.digits = p.digits;
   a.chunk = p.chunk;
   a.chunks = p.chunks;
+  a.once = a.cols * (a.tokens * (a.out_f32 ? 4 : 2) + a.vocab * (a.grad_f32 ? 4 : 2)) > kOnceBwd;
   // Rows that the sort's launches write zeros to: as many as take about the time of the sort.
   const int64_t row_bytes = (int64_t)a.cols * (a.grad_f32 ? 4 : 2), most = p.blocks == 1 ? kFillOne : kFillPass * p.passes;
   a.filled = a.add ? a.vocab : std::max<int64_t>(0, a.vocab - most / row_bytes);
@@ -600,12 +624,14 @@ hipError_t launch_embedding_bwd(EmbeddingArgs a, hipStream_t s) {
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(sums + fill), dim3(threads), 0, s, a, sums, across); };
     using D = decltype(d);
     using G = decltype(g);
-    if (least <= 32)
-      launch(embedding_sum_kernel<D, G, false, true>);
-    else if (a.cols % Form<D, G>::N)
-      launch(embedding_sum_kernel<D, G, true, true>);
+    if (least <= 32) return launch(embedding_sum_kernel<D, G, false, true, false>);
+    if constexpr (kWholeLines<D, G>)
+      if (a.once)
+        return a.cols % Form<D, G>::N ? launch(embedding_sum_kernel<D, G, true, true, true>) : launch(embedding_sum_kernel<D, G, true, false, true>);
+    if (a.cols % Form<D, G>::N)
+      launch(embedding_sum_kernel<D, G, true, true, false>);
     else
-      launch(embedding_sum_kernel<D, G, true, false>);
+      launch(embedding_sum_kernel<D, G, true, false, false>);
   });
   if (p.chunks > 1) {
     const dim3 grid(p.chunks, (a.cols + 255) / 256), block(kJoinThreads, kJoinRuns);

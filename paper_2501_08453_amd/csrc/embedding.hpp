@@ -17,6 +17,7 @@ struct EmbeddingArgs {
   int cols;
   float scale;
   bool ids64, table_f32, out_f32, grad_f32, add;
+  bool once;                 // backward: zeros and dout past the caches
   // backward: the tokens' ids in order, and where they stand; two of each, as a pass of the sort goes from one to the other
   uint32_t *keys[2], *pos[2];
   uint32_t* hist;            // [blocks][512] digits of a pass, where several workgroups sort

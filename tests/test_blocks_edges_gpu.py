@@ -173,3 +173,28 @@ def test_more_columns_than_32_bits_hold():
               lambda: vc.embedding_fwd(ids, wide, out=wide), lambda: vc.embedding_bwd(wide, ids, 1, into=wide)):
         with pytest.raises((ValueError, vc.JointAttnError), match="invalid descriptor|SHAPE|shape"):  # the backward asks for a workspace first
             f()
+
+
+@pytest.mark.parametrize("cols,t,grad", [(4800, "f32", "f32"), (4801, "f32", "f32"), (4800, "bf16", "f32"), (4803, "bf16", "bf16"), (4800, "f32", "bf16")])
+def test_embedding_of_more_than_the_caches_hold(cols, t, grad):
+    """Lookups and gradients large enough to go past the caches: u = 2^-24, a row's sum of n tokens is off by (n + 18) u of the
+    magnitudes, and half a step of its type."""
+    import torch
+    vc = _vc()
+    dt = {"f32": torch.float32, "bf16": torch.bfloat16}
+    T, V = (16001 if t == "f32" else 30001), 900
+    ids = torch.randint(-1, V, (T,), device="cuda")
+    ids[::7] = 3
+    table, dout = torch.randn((V, cols), device="cuda").to(dt[t]), torch.randn((T, cols), device="cuda").to(dt[t])
+    real = (ids >= 0) & (ids != 5)
+    want = torch.where(real[:, None], table[ids.clamp(min=0)] * 0.5, torch.zeros((), dtype=dt[t], device="cuda"))
+    assert torch.equal(vc.embedding_fwd(ids, table, 0.5, 5), want)  # a half is exact
+    got = vc.embedding_bwd(dout, ids, V, 0.5, 5, dtype=dt[grad])
+    n = torch.bincount(ids[real], minlength=V)[:, None]
+    half = 2.0 ** -8 if grad == "bf16" else 2.0 ** -24
+    for c in range(0, cols, 1601):
+        d = dout[real][:, c:c + 1601].double()
+        s, mag = (torch.zeros((V, d.shape[1]), dtype=torch.float64, device="cuda").index_add_(0, ids[real], 0.5 * p) for p in (d, d.abs()))
+        tol = (n + 18) * 2.0 ** -24 * mag
+        assert ((got[:, c:c + 1601].double() - s).abs() <= tol + half * (s.abs() + tol)).all()
+    assert not got[5].any() and torch.equal(got, vc.embedding_bwd(dout, ids, V, 0.5, 5, dtype=dt[grad]))
