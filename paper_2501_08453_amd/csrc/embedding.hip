@@ -21,11 +21,11 @@ constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kOneBlock = 8192;   // most tokens that one workgroup sorts
 constexpr int kFillRows = 64;      // rows of the table that a workgroup looks through for zeros
-// Bytes of zeros beside the sort of one workgroup, or beside a pass of several, and most workgroups that write them. 65,536 tokens, 50,000 x
-// 1,536 in fp32, two passes, bf16 rows, ids as words come (15,644 of them met): 65 MB a pass 245 us in all with the lookup, 98 MB 233, 131 MB 227,
-// 154 MB (the whole table) 231; none 285. Where nearly every row is met, what was written beside the sort is written twice: 131 MB a pass cost
-// 50 us of 208 there.
-constexpr int64_t kFillOne = (int64_t)128 << 20, kFillPass = (int64_t)128 << 20;
+// Bytes of zeros beside the sort of one workgroup, or beside a pass of several, and most workgroups that write them. Lookup and gradient
+// with ids as words come, bf16 rows, fp32 gradients of 1,536 columns, at 16, 32, 64, 96 and 128 MiB a pass: 65,536 tokens of 50,000 ids 180,
+// 176, 176, 173 and 171 us, of 32,128 162, 159, 147, 153 and 153, 16,384 of 50,000 121, 117, 109, 104 and 108. (Where nearly every row is met, what
+// was written beside the sort is written twice.)
+constexpr int64_t kFillOne = (int64_t)128 << 20, kFillPass = (int64_t)96 << 20;
 constexpr int kFillGroups = 512;
 
 // The ids of K tokens at(0), at(1), ..., all in flight at once (so no branch stands between two of them, and every place exists);
@@ -348,7 +348,7 @@ __device__ __forceinline__ void write_row(const EmbeddingArgs& a, int64_t id, co
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0), the other counters as they are
 
 // Zeros to those of the rows [v0, v0 + kFillRows) before `filled` that no token met.
-template <class G>
+template <class G, bool ONCE>
 __device__ __forceinline__ void fill_unmet(const EmbeddingArgs& a, int64_t v0) {
   const uint32_t* keys = a.keys[0];
   const int waves = blockDim.x >> 6, lane = threadIdx.x & 63;
@@ -364,7 +364,7 @@ __device__ __forceinline__ void fill_unmet(const EmbeddingArgs& a, int64_t v0) {
   for (int i = 0; rows; ++i, rows &= rows - 1) {
     if (i % waves != (int)(threadIdx.x >> 6)) continue;
     G* g = (G*)a.grad + (v0 + __ffsll((unsigned long long)rows) - 1) * a.cols;
-    for (int c = lane * M; c < a.cols; c += 64 * M) store_cols(g, zero, span_at<M>(c, a.cols));
+    for (int c = lane * M; c < a.cols; c += 64 * M) store_cols<true, ONCE>(g, zero, span_at<M>(c, a.cols));
   }
 }
 
@@ -375,7 +375,7 @@ __device__ __forceinline__ void fill_unmet(const EmbeddingArgs& a, int64_t v0) {
 template <class D, class G, bool WHOLE, bool ODD, bool ONCE>
 __global__ __launch_bounds__(1024) void embedding_sum_kernel(EmbeddingArgs a, int sums, int across) {
   constexpr int N = Form<D, G>::N, V = Form<D, G>::V, U = WHOLE && !ODD && sizeof(D) == 2 ? 16 : 8;  // U: rows of a thread in flight
-  if ((int)blockIdx.x >= sums) return fill_unmet<G>(a, ((int64_t)blockIdx.x - sums) * kFillRows);
+  if ((int)blockIdx.x >= sums) return fill_unmet<G, ONCE>(a, ((int64_t)blockIdx.x - sums) * kFillRows);
   const uint32_t *keys = a.keys[0], *pos = a.pos[0];
   const uint32_t none = (uint32_t)a.vocab;
   const int64_t T = a.tokens;
