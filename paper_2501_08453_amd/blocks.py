@@ -141,6 +141,14 @@ def _type(name, t):
     return k
 
 
+def _new(t, shape, dtype, device):
+    """A contiguous tensor; of one that is just so and at hand it takes less time."""
+    import torch
+    if t is not None and t.dtype is dtype and t.is_contiguous():
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+    return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _vector(name, p, cols, S, every, dtype):
     """Appends a parameter to the checks; its stride between samples."""
     if p.dim() == 1:
@@ -226,10 +234,10 @@ def residual_norm_fwd(x, a, desc, gate=None, scale=None, shift=None, post_weight
     d = _residual_desc(desc, x, a, gate, scale, shift, post_weight, cu, lens, y_type)
     rows, cols, dev = d.rows, d.cols, x.device
     shape = (rows, cols)
-    h = None if a is None else torch.empty(shape, dtype=x.dtype, device=dev)
+    h = None if a is None else _new(x, shape, x.dtype, dev)
     y = stats = h8 = a8 = None
     if d.norm:
-        y = torch.empty(shape, dtype=y_dtype, device=dev)
+        y = _new(x if a is None else a, shape, y_dtype, dev)
     if d.norm or d.post_norm:
         stats = torch.empty((4, rows), dtype=torch.float32, device=dev)
     if d.checkpoint:
@@ -291,13 +299,13 @@ def residual_norm_bwd(dh, dy, saved, ws=None, want=(True,) * 6):
         every.append(("saved.lens", s.lens, (d.samples,), torch.int32, False))
     _check_all(every)
     dev = every[0][1].device
-    dx = torch.empty(shape, dtype=types[d.x_type], device=dev) if want[0] else None
-    da = torch.empty(shape, dtype=types[d.y_type], device=dev) if a is not None and want[1] else None
+    dx = _new(dh, shape, types[d.x_type], dev) if want[0] else None
+    da = _new(dy, shape, types[d.y_type], dev) if a is not None and want[1] else None
     vectors, sums = [], False
     for p, w in zip((s.gate, s.scale, s.shift, s.post_weight), want[2:]):
         g = None
         if p is not None and w:
-            g, sums = torch.empty(p.shape, dtype=p.dtype, device=dev), True
+            g, sums = _new(p, p.shape, p.dtype, dev), True
         vectors.append(g)
     if dx is None and da is None and not sums:
         return (None,) * 6
@@ -328,15 +336,16 @@ def checkpoint_pack(x, out=None):
     import torch
     f32 = _type("x", x)
     rows, cols, stride = _rows_of(x)
-    kept, blocks = out, x.shape[:-1] + ((cols + BLOCK - 1) // BLOCK,)
+    shape = x.shape
+    kept, blocks = out, (*shape[:-1], (cols + BLOCK - 1) // BLOCK)
     if out is None:
-        _check_all([("x", x, x.shape, x.dtype, True)])
-        kept = Packed8(torch.empty(x.shape, dtype=torch.int8, device=x.device),
+        _check_all([("x", x, shape, x.dtype, True)])
+        kept = Packed8(torch.empty_like(x, dtype=torch.int8, memory_format=torch.contiguous_format),
                        torch.empty(blocks, dtype=torch.float32, device=x.device), x.dtype)
     elif out.dtype is not x.dtype:
         raise ValueError("out is of %s, x of %s" % (out.dtype, x.dtype))
     else:
-        _check_all([("x", x, x.shape, x.dtype, True), ("out.q", out.q, x.shape, torch.int8, False),
+        _check_all([("x", x, shape, x.dtype, True), ("out.q", out.q, shape, torch.int8, False),
                     ("out.scales", out.scales, blocks, torch.float32, False)])
     if rows:
         _call_on(x.device, "vc_checkpoint_pack", vc_checkpoint_desc(rows, min(cols, _COLS), f32, stride), x, kept.q, kept.scales)
@@ -349,13 +358,14 @@ def checkpoint_unpack(kept, dtype=None, out=None):
     q, scales = kept.q, kept.scales
     rows, cols, _ = _rows_of(q)
     if out is None:
-        out = torch.empty(q.shape, dtype=kept.dtype if dtype is None else dtype, device=q.device)
+        out = torch.empty_like(q, dtype=kept.dtype if dtype is None else dtype, memory_format=torch.contiguous_format)
     elif dtype is not None and out.dtype is not dtype:
         raise ValueError("out must be %s, got %s" % (dtype, out.dtype))
     f32 = _type("out", out)
-    _check_all([("q", q, q.shape, torch.int8, False),
-                ("scales", scales, q.shape[:-1] + ((cols + BLOCK - 1) // BLOCK,), torch.float32, False),
-                ("out", out, q.shape, out.dtype, False)])
+    shape = q.shape
+    _check_all([("q", q, shape, torch.int8, False),
+                ("scales", scales, (*shape[:-1], (cols + BLOCK - 1) // BLOCK), torch.float32, False),
+                ("out", out, shape, out.dtype, False)])
     if rows:
         _call_on(q.device, "vc_checkpoint_unpack", vc_checkpoint_desc(rows, min(cols, _COLS), f32, 0), q, scales, out)
     return out
@@ -399,13 +409,14 @@ def embedding_fwd(ids, table, scale=1.0, padding_id=None, dtype=None, out=None):
     if table.dim() != 2:
         raise ValueError("table has shape %s, expected [vocab, columns]" % (tuple(table.shape),))
     V, cols = table.shape
+    shape = (*ids.shape, cols)
     if out is None:
-        out = torch.empty(ids.shape + (cols,), dtype=table.dtype if dtype is None else dtype, device=table.device)
+        out = torch.empty(shape, dtype=table.dtype if dtype is None else dtype, device=table.device)
     elif dtype is not None and out.dtype is not dtype:
         raise ValueError("out must be %s, got %s" % (dtype, out.dtype))
     of = _type("out", out)
     _check_all([("ids", ids, ids.shape, ids.dtype, False), ("table", table, (V, cols), table.dtype, True),
-                ("out", out, ids.shape + (cols,), out.dtype, False)])
+                ("out", out, shape, out.dtype, False)])
     desc = vc_embedding_desc(ids.numel(), V, -1 if padding_id is None else padding_id, _row_stride("table", table), min(cols, _COLS), i64, tf,
                              of, scale, 0)
     if desc.tokens:
@@ -427,7 +438,7 @@ def embedding_bwd(dout, ids, vocab, scale=1.0, padding_id=None, dtype=None, into
     else:
         grad = into
     gf = _type("dtable", grad)
-    _check_all([("dout", dout, ids.shape + (cols,), dout.dtype, True), ("ids", ids, ids.shape, ids.dtype, False),
+    _check_all([("dout", dout, (*ids.shape, cols), dout.dtype, True), ("ids", ids, ids.shape, ids.dtype, False),
                 ("into", grad, (vocab, cols), grad.dtype, False)])
     desc = vc_embedding_desc(ids.numel(), vocab, -1 if padding_id is None else padding_id, _row_stride("dout", dout), min(cols, _COLS), i64,
                              gf, of, scale, 0 if into is None else 1)
