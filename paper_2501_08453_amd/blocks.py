@@ -155,11 +155,14 @@ def _vector(name, p, cols, S, every, dtype):
         every.append((name, p, (cols,), dtype, False))
         return SHARED
     every.append((name, p, (S, cols), dtype, True))
-    if p.is_contiguous() or S == 1 and p.stride(-1) == 1:
+    if p.is_contiguous():
         return 0
-    if p.dim() != 2 or p.stride(1) != 1 or p.stride(0) < cols:
+    strides = p.stride()
+    if S == 1 and strides[-1] == 1:
+        return 0
+    if len(strides) != 2 or strides[1] != 1 or strides[0] < cols:
         raise ValueError("%s must be [columns], or [samples, columns] with contiguous rows" % name)
-    return p.stride(0)
+    return strides[0]
 
 
 def _vectors(d, every, gate, scale, shift, post_weight):
