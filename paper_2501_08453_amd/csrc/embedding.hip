@@ -4,7 +4,7 @@
 //
 // Bound by memory: rows of the table, rows of dout, and every row of the gradient, which is written whole (zeros where no token met it).
 // Sort: digits of up to nine bits, the last first. A wave finds the lanes of the same digit by ballots and counts for itself, so that
-// the order is that of the tokens. Up to 8,192 tokens one workgroup sorts in LDS; more take two launches a digit.
+// the order is that of the tokens. Up to 8,192 tokens one workgroup sorts in LDS; more take two launches a digit. Up to 64 need no sort.
 // Sums: a share of the sorted list writes the rows of ids that begin and end in it; the sums of ids that go on beyond it are
 // kept apart and added in order by the last kernel, however many shares a frequent id fills.
 // 65,536 tokens of 50,000 ids as words come, 1,536 columns, bf16 rows, fp32 gradient: lookup 47 us (5.3 TB/s), sort and zeros 44, sums 71, joins 10.
@@ -21,6 +21,10 @@ constexpr int kRowThreads = 256;   // threads of a workgroup, where a row takes 
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kOneBlock = 8192;   // most tokens that one workgroup sorts
+constexpr int kFewTokens = 64;    // most that need no sort
+// Bytes of zeros of a workgroup then. 64 tokens of 2,000 ids of 2,048 columns in fp32, 50,000 of 1,536, 100,000 of 64: 9, 64 and 15 us on the GPU, with
+// 16 KiB 12, 134 and 15; by three launches 12, 67 and 14, and 17 us of the host for a small call instead of 11.
+constexpr int64_t kFewFill = 65536;
 constexpr int kFillRows = 64;      // rows of the table that a workgroup looks through for zeros
 // Bytes of zeros beside the sort of one workgroup, or beside a pass of several, and most workgroups that write them. Lookup and gradient
 // with ids as words come, bf16 rows, fp32 gradients of 1,536 columns, at 16, 32, 64, 96 and 128 MiB a pass: 65,536 tokens of 50,000 ids 180,
@@ -348,25 +352,79 @@ __device__ __forceinline__ void write_row(const EmbeddingArgs& a, int64_t id, co
 // keys say: left to itself, the compiler waits for everything, the stores' round trips too, before each next token.
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0), the other counters as they are
 
-// Zeros to those of the rows [v0, v0 + kFillRows) before `filled` that no token met.
+// Zeros to those of the rows [v0, v0 + kFillRows) whose lane says that no token met them.
 template <class G, bool ONCE>
-__device__ __forceinline__ void fill_unmet(const EmbeddingArgs& a, int64_t v0) {
-  const uint32_t* keys = a.keys[0];
+__device__ __forceinline__ void zero_rows(const EmbeddingArgs& a, int64_t v0, bool unmet) {
   const int waves = blockDim.x >> 6, lane = threadIdx.x & 63;
-  const int64_t id = v0 + lane;
-  bool unmet = false;
-  if (id < a.filled) {
-    const int64_t i = lower(keys, 0, a.tokens, (uint32_t)id);
-    unmet = i == a.tokens || keys[i] != (uint32_t)id;
-  }
   uint64_t rows = __ballot(unmet);
   constexpr int M = 16 / sizeof(G);
   const float zero[M] = {};
+  if (a.cols % M == 0) {  // rows of whole vectors: one behind the other
+    const int per = a.cols / M, n = rows ? (64 - __builtin_clzll(rows)) * per : 0;
+    G* g = (G*)a.grad + v0 * a.cols;
+    for (int i = threadIdx.x; i < n; i += blockDim.x)
+      if (rows >> (i / per) & 1) put<ONCE, M>(g + (int64_t)i * M, zero);
+    return;
+  }
   for (int i = 0; rows; ++i, rows &= rows - 1) {
     if (i % waves != (int)(threadIdx.x >> 6)) continue;
     G* g = (G*)a.grad + (v0 + __ffsll((unsigned long long)rows) - 1) * a.cols;
     for (int c = lane * M; c < a.cols; c += 64 * M) store_cols<true, ONCE>(g, zero, span_at<M>(c, a.cols));
   }
+}
+
+// ... of those before `filled`, by the sorted tokens.
+template <class G, bool ONCE>
+__device__ __forceinline__ void fill_unmet(const EmbeddingArgs& a, int64_t v0) {
+  const uint32_t* keys = a.keys[0];
+  const int64_t id = v0 + (threadIdx.x & 63);
+  bool unmet = false;
+  if (id < a.filled) {
+    const int64_t i = lower(keys, 0, a.tokens, (uint32_t)id);
+    unmet = i == a.tokens || keys[i] != (uint32_t)id;
+  }
+  zero_rows<G, ONCE>(a, v0, unmet);
+}
+
+// Up to 64 tokens, without a sort: every wave has all of them in its lanes. A workgroup for each token sums the rows of all that
+// have its id, in order, if it is the first of these; the others write zeros to `fill` rows each.
+template <class D, class G, bool ONCE>
+__global__ __launch_bounds__(1024) void embedding_few_kernel(EmbeddingArgs a, int fill) {
+  constexpr int N = Form<D, G>::N, V = Form<D, G>::V, U = 8;  // U: rows of a thread in flight
+  const int T = (int)a.tokens, lane = threadIdx.x & 63, t = blockIdx.x;
+  uint32_t key[1];
+  ids_of<1>(a, key, [&](int) { return (int64_t)min(lane, T - 1); });
+  if (t >= T) {
+    const int64_t v0 = (int64_t)(t - T) * fill, id = v0 + lane;
+    bool unmet = lane < fill && id < a.vocab;
+    for (int j = 0; j < T; ++j) unmet = unmet && (uint32_t)__builtin_amdgcn_readlane(key[0], j) != (uint32_t)id;
+    return zero_rows<G, ONCE>(a, v0, unmet);
+  }
+  const uint32_t id = __builtin_amdgcn_readlane(key[0], t);
+  uint64_t mine = __ballot(lane < T && key[0] == id);
+  if (id >= (uint32_t)a.vocab || __ffsll((unsigned long long)mine) - 1 != t) return;
+  Span<N> s[V];
+  spans_of<N, V>(s, threadIdx.x, blockDim.x, a.cols);
+  float sum[8] = {};
+  while (mine) {
+    const int n = __popcll(mine);
+    Cols<D, N> r[U][V];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = mine ? __ffsll((unsigned long long)mine) - 1 : t;  // behind the last, one that is there already
+      mine &= mine - 1;
+#pragma unroll
+      for (int v = 0; v < V; ++v) load_cols(r[u][v], (const D*)a.dout + at * a.dout_stride, s[v]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u < n)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int e = 0; e < N; ++e) sum[N * v + e] += r[u][v][e];
+  }
+  write_row<G, N, V>(a, id, s, sum);
 }
 
 // The first `sums` workgroups sum shares of the sorted tokens, the others write zeros. `across` threads a share; WHOLE: these are whole
@@ -578,6 +636,20 @@ hipError_t launch_embedding_bwd(EmbeddingArgs a, hipStream_t s) {
   a.chunk = p.chunk;
   a.chunks = p.chunks;
   a.once = a.cols * (a.tokens * (a.out_f32 ? 4 : 2) + a.vocab * (a.grad_f32 ? 4 : 2)) > kOnceBwd;
+  if (a.tokens <= kFewTokens) {
+    const int threads = std::max(kRowThreads, ((a.cols + 7) / 8 + 63) / 64 * 64);
+    const int64_t row_bytes = (int64_t)a.cols * (a.grad_f32 ? 4 : 2);
+    const int fill = (int)std::min<int64_t>(64, std::max<int64_t>(1, kFewFill / row_bytes));
+    const dim3 grid(a.tokens + (a.add ? 0 : (a.vocab + fill - 1) / fill));
+    pick(a.out_f32, a.grad_f32, [&](auto d, auto g) {
+      auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a, fill); };
+      if (a.once)
+        launch(embedding_few_kernel<decltype(d), decltype(g), true>);
+      else
+        launch(embedding_few_kernel<decltype(d), decltype(g), false>);
+    });
+    return hipGetLastError();
+  }
   // Rows that the sort's launches write zeros to: as many as take about the time of the sort.
   const int64_t row_bytes = (int64_t)a.cols * (a.grad_f32 ? 4 : 2), most = p.blocks == 1 ? kFillOne : kFillPass * p.passes;
   a.filled = a.add ? a.vocab : std::max<int64_t>(0, a.vocab - most / row_bytes);

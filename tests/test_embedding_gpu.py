@@ -179,3 +179,11 @@ def test_differentiable_graph_and_stream():
             g.replay()
             torch.cuda.synchronize()
             assert torch.equal(o, vc.embedding_fwd(ids, table, 2.0, 3)) and torch.equal(d, vc.embedding_bwd(dout, ids, 257, 2.0, 3))
+
+
+@pytest.mark.parametrize("how", ["spread", "often", "one", "none"])
+@pytest.mark.parametrize("tokens", [1, 2, 8, 9, 63, 64, 65])
+def test_few_tokens(tokens, how):
+    """Up to 64 tokens there is no sort: rows of one vector, of several waves, with odd ends; more ids than a workgroup clears."""
+    for vocab, cols, t in ((3, 5, "f32"), (130, 2056, "bf16"), (700, 1027, "bf16"), (5000, 64, "f32")):
+        check(*make(tokens, vocab, cols, t, ids="i32" if tokens % 2 else "i64", how=how), scale=0.75, padding=2)
