@@ -636,13 +636,13 @@ hipError_t launch_embedding_bwd(EmbeddingArgs a, hipStream_t s) {
   a.chunk = p.chunk;
   a.chunks = p.chunks;
   a.once = a.cols * (a.tokens * (a.out_f32 ? 4 : 2) + a.vocab * (a.grad_f32 ? 4 : 2)) > kOnceBwd;
-  if (a.tokens <= kFewTokens) {
-    const int threads = std::max(kRowThreads, ((a.cols + 7) / 8 + 63) / 64 * 64);
-    const int64_t row_bytes = (int64_t)a.cols * (a.grad_f32 ? 4 : 2);
-    const int fill = (int)std::min<int64_t>(64, std::max<int64_t>(1, kFewFill / row_bytes));
-    const dim3 grid(a.tokens + (a.add ? 0 : (a.vocab + fill - 1) / fill));
+  const int64_t row_bytes = (int64_t)a.cols * (a.grad_f32 ? 4 : 2);
+  const int few_threads = std::max(kRowThreads, ((a.cols + 7) / 8 + 63) / 64 * 64);
+  const int fill_each = (int)std::min<int64_t>(64, std::max<int64_t>(1, kFewFill / row_bytes));
+  const int64_t few_groups = a.tokens + (a.add ? 0 : (a.vocab + fill_each - 1) / fill_each);
+  if (a.tokens <= kFewTokens && few_groups * few_threads < (int64_t)1 << 32) {  // a launch has less threads than that
     pick(a.out_f32, a.grad_f32, [&](auto d, auto g) {
-      auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a, fill); };
+      auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(few_groups), dim3(few_threads), 0, s, a, fill_each); };
       if (a.once)
         launch(embedding_few_kernel<decltype(d), decltype(g), true>);
       else
@@ -651,7 +651,7 @@ hipError_t launch_embedding_bwd(EmbeddingArgs a, hipStream_t s) {
     return hipGetLastError();
   }
   // Rows that the sort's launches write zeros to: as many as take about the time of the sort.
-  const int64_t row_bytes = (int64_t)a.cols * (a.grad_f32 ? 4 : 2), most = p.blocks == 1 ? kFillOne : kFillPass * p.passes;
+  const int64_t most = p.blocks == 1 ? kFillOne : kFillPass * p.passes;
   a.filled = a.add ? a.vocab : std::max<int64_t>(0, a.vocab - most / row_bytes);
   auto fills = [&](int64_t rows) { return (int)std::min<int64_t>(kFillGroups, (rows * row_bytes + 65535) / 65536); };
   if (p.blocks == 1) {
