@@ -208,7 +208,9 @@ vc_status vc_residualnorm_bwd(const vc_residualnorm_desc* desc, const void* dh, 
   r.dwp = dpost_weight;
   if (sums) {
     r.part = static_cast<float*>(workspace);
-    r.flat = desc->samples == 1 || !(gate && r.gate_stride || dscale && r.scale_stride || dshift && r.shift_stride);
+    // a gate's gradient may be wanted where the gate itself is not given (1); a gate of each sample weighs the sums of dpost_weight
+    const bool own = (gate || dgate) && r.gate_stride || dscale && r.scale_stride || dshift && r.shift_stride;
+    r.flat = desc->samples == 1 || !own;
     if (!r.flat && (dpost_weight || (dgate && !r.gate_stride) || (dscale && !r.scale_stride) || (dshift && !r.shift_stride)))
       r.sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_bytes(desc));
   }
