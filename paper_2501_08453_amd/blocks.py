@@ -384,7 +384,7 @@ def saved_in_8bit(min_elements=1 << 16):
     def pack(t):
         if (t.device.type != "cuda" or t.dtype is not torch.bfloat16 or t.dim() < 2 or
                 t.numel() < min_elements or (t if t._base is None else t._base).is_leaf or t.shape[-1] < 64 or not t.is_contiguous()):
-            return t
+            return t.detach()  # a result that its operation saves would hold that operation, and itself through it
         return checkpoint_pack(t.detach())
 
     def unpack(t):

@@ -1,0 +1,38 @@
+"""saved_in_8bit on the CPU, where nothing is packed: what it keeps is what autograd keeps without it."""
+import gc
+import weakref
+
+import pytest
+
+import paper_2501_08453_amd as vc
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.mark.parametrize("op", [torch.exp, lambda t: t.softmax(-1), lambda t: t.sigmoid() * t, lambda t: t[:, :3].tanh()])
+def test_a_graph_that_is_dropped_is_freed(op):
+    """An operation that saves its own result holds it; kept as it is, the result would hold the operation in turn."""
+    gone = []
+    for context in (torch.enable_grad, vc.saved_in_8bit):
+        x = torch.randn((4, 70), requires_grad=True)
+        with context():
+            y = op(x)
+        ref = weakref.ref(y)
+        del y
+        gc.collect()
+        gone.append(ref() is None)
+    assert gone == [True, True]
+
+
+def test_gradients_of_what_is_not_packed():
+    """Those without the context, of the first and of the second order."""
+    x = torch.randn((5, 70), dtype=torch.float64, requires_grad=True)
+    w = torch.randn((70, 66), dtype=torch.float64, requires_grad=True)
+    got = []
+    for context in (torch.enable_grad, vc.saved_in_8bit):
+        with context():
+            y = ((x * 2).exp() @ w).softmax(-1)
+            g = torch.autograd.grad((y * y).sum(), (x, w), create_graph=True)
+            gg = torch.autograd.grad(sum((t * t).sum() for t in g), (x, w))
+        got.append(g + gg)
+    assert all(torch.equal(a, b) for a, b in zip(*got))
