@@ -374,6 +374,12 @@ def checkpoint_unpack(kept, dtype=None, out=None):
     return out
 
 
+class _Whole(NamedTuple):
+    """A saved tensor as it is, and how often it had been changed in place."""
+    tensor: object
+    version: int
+
+
 def saved_in_8bit(min_elements=1 << 16):
     """A context in which autograd keeps activations in 8 bits: contiguous tensors of bf16, of at least min_elements elements, two
     dimensions and 64 columns, that an operation saves for its backward are packed, and unpacked where the backward asks for
@@ -384,11 +390,15 @@ def saved_in_8bit(min_elements=1 << 16):
     def pack(t):
         if (t.device.type != "cuda" or t.dtype is not torch.bfloat16 or t.dim() < 2 or
                 t.numel() < min_elements or (t if t._base is None else t._base).is_leaf or t.shape[-1] < 64 or not t.is_contiguous()):
-            return t.detach()  # a result that its operation saves would hold that operation, and itself through it
+            return _Whole(t.detach(), t._version)  # a result that its operation saves would hold that operation, and itself through it
         return checkpoint_pack(t.detach())
 
-    def unpack(t):
-        return checkpoint_unpack(t) if isinstance(t, Packed8) else t
+    def unpack(kept):
+        if isinstance(kept, Packed8):
+            return checkpoint_unpack(kept)
+        if kept.tensor._version != kept.version:  # autograd itself does not look where there are hooks
+            raise RuntimeError("a tensor %s that an operation saved for its backward was changed in place since" % (tuple(kept.tensor.shape),))
+        return kept.tensor
 
     return torch.autograd.graph.saved_tensors_hooks(pack, unpack)
 

@@ -36,3 +36,38 @@ def test_gradients_of_what_is_not_packed():
             gg = torch.autograd.grad(sum((t * t).sum() for t in g), (x, w))
         got.append(g + gg)
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_changed_in_place_after_it_was_saved():
+    """Hooks switch off autograd's own check: without another, the backward would go on with the changed values."""
+    x = torch.randn((4, 70), requires_grad=True)
+    w = torch.randn((70, 70), requires_grad=True)
+
+    def result(a):
+        y = a.exp()
+        y.add_(1)
+        return y
+
+    def operand(a):
+        u = a * 2
+        y = u * u
+        u[1:].zero_()
+        return y
+
+    def weight(a):
+        y = a @ w
+        with torch.no_grad():
+            w.mul_(0.5)
+        return y
+
+    for f in (result, operand, weight):
+        with vc.saved_in_8bit():
+            y = f(x)
+        with pytest.raises(RuntimeError, match="in place"):
+            torch.autograd.grad(y.sum(), x)
+    with vc.saved_in_8bit():  # before it is saved, and what nobody saves, may change
+        u = x * 2
+        u.add_(1)
+        y = u.exp() + 0
+        y.mul_(3)
+    assert torch.equal(torch.autograd.grad(y.sum(), x)[0], 6 * (2 * x.detach() + 1).exp())
