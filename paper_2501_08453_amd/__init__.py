@@ -577,6 +577,16 @@ def temporal_bwd(q, k, v, o, lse, dout, desc, key_mask=None, ws=None):
     return dq, dk, dv
 
 
+def _save_whole(*tensors):
+    """Marks tensors that an operation saves for its backward and that saved_in_8bit is to leave as they are: q, k and the bias of an
+    attention, whose probabilities the backward computes again with the exact log-sum-exps. From 8 bits, rows of sharp
+    probabilities would not add up to 1 (logits of a standard deviation of 4, 8, 16: sums of 0.91 to 1.13, 0.80 to 1.22, 0.66 to 1.45,
+    gradients off by 4, 8, 17%; with q and k as they are by 1.6, 2.2, 2.9%)."""
+    for t in tensors:
+        if t is not None and not t.is_leaf:  # leaves stay anyway
+            t._vc_save_whole = True
+
+
 _AUTOGRAD = {}
 
 
@@ -608,6 +618,7 @@ def _autograd_functions():
         @staticmethod
         def forward(ctx, q, k, v, desc, branch, text_len=None, key_mask=None):
             o, lse = branch_fwd(branch, q, k, v, desc, text_len, key_mask)
+            _save_whole(q, k)
             ctx.save_for_backward(q, k, v, o, lse)
             ctx.desc, ctx.branch, ctx.text_len, ctx.key_mask = desc, branch, text_len, key_mask
             return o
@@ -630,6 +641,7 @@ def _autograd_functions():
             o_j, l_j = fwd(q, k, v, desc, text_len, key_mask)
             o_s, l_s = spatial_fwd(q, k, v, desc, text_len, key_mask)
             o_t, l_t, out = temporal_fwd_sum(q, k, v, desc, o_joint=o_j, o_spatial=o_s, key_mask=key_mask)
+            _save_whole(q, k)
             ctx.save_for_backward(q, k, v, o_j, l_j, o_s, l_s, o_t, l_t)
             ctx.desc, ctx.text_len, ctx.key_mask = desc, text_len, key_mask
             return out

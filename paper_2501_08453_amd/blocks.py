@@ -384,12 +384,14 @@ def saved_in_8bit(min_elements=1 << 16):
     """A context in which autograd keeps activations in 8 bits: contiguous tensors of bf16, of at least min_elements elements, two
     dimensions and 64 columns, that an operation saves for its backward are packed, and unpacked where the backward asks for
     them. Leaves (parameters, inputs) and views of them stay as they are, for they are kept anyway, and so do tensors of 32 bits
-    (log-sum-exps, statistics). A tensor that several operations save is packed for each of them. An attention's backward then computes its probabilities from the kept q and k."""
+    (log-sum-exps, statistics). A tensor that several operations save is packed for each of them. Of an attention of this package v
+    and o are packed; q, k and a bias stay, since the backward computes the probabilities again from them with the exact log-sum-exps.
+    A fused attention of another origin that does the same does not belong in the context: it cannot be told from other operations here."""
     import torch
 
     def pack(t):
         if (t.device.type != "cuda" or t.dtype is not torch.bfloat16 or t.dim() < 2 or
-                t.numel() < min_elements or (t if t._base is None else t._base).is_leaf or t.shape[-1] < 64 or not t.is_contiguous()):
+                t.numel() < min_elements or hasattr(t, "_vc_save_whole") or (t if t._base is None else t._base).is_leaf or t.shape[-1] < 64 or not t.is_contiguous()):
             return _Whole(t.detach(), t._version)  # a result that its operation saves would hold that operation, and itself through it
         return checkpoint_pack(t.detach())
 

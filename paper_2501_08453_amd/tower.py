@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 
-from paper_2501_08453_amd import (_call, _check_placed, _check_shape, _lib, _ptr, _stream, _workspace,
+from paper_2501_08453_amd import (_call, _check_placed, _check_shape, _lib, _ptr, _save_whole, _stream, _workspace,
                                   vc_layernorm_desc, vc_packedattn_desc)
 
 MAX_DISTANCE = 512   # largest max_distance of a bias (VC_ERR_SHAPE beyond)
@@ -317,6 +317,7 @@ def _autograd_functions():
         @staticmethod
         def forward(ctx, q, k, v, bias, desc, cu_q, cu_k, len_q, len_k, buckets):
             o, lse = packed_fwd(q, k, v, desc, cu_q, cu_k, len_q, len_k, bias, buckets)
+            _save_whole(q, k, bias)
             ctx.save_for_backward(q, k, v, bias, o, lse, cu_q, cu_k, len_q, len_k, buckets)
             ctx.desc = vc_packedattn_desc.from_buffer_copy(desc)  # the caller may change theirs before the backward
             return o

@@ -1,0 +1,69 @@
+"""saved_in_8bit on the GPU: which tensors it leaves as they are, for their operation's sake."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+SHARP = 16.0  # of q: logits of a standard deviation of 16
+
+
+def _vc():
+    import paper_2501_08453_amd as vc
+    return vc
+
+
+def _leaves(*shape, n=3):
+    import torch
+    return [torch.randn(shape, device="cuda").to(torch.bfloat16).requires_grad_(True) for _ in range(n)]
+
+
+def _through(t):
+    vc = _vc()
+    return vc.checkpoint_unpack(vc.checkpoint_pack(t.detach()))
+
+
+@pytest.mark.parametrize("branch", ["joint", "spatial", "temporal", "block"])
+def test_queries_and_keys_of_an_attention_stay(branch):
+    """The backward computes the probabilities of exact log-sum-exps: from q and k in 8 bits rows of sharp ones would not add up to 1 (0.66
+    to 1.45 at a deviation of 16). v and o may be packed: bit by bit the gradients of that."""
+    import torch
+    vc = _vc()
+    desc = vc.make_desc(1, 2, 64, 64, 2, 16, 16, deterministic=True)
+    leaves = _leaves(1, 64 + 2 * 256, 2, 64)
+    do = torch.randn(leaves[0].shape, device="cuda").to(torch.bfloat16)
+    scaled = lambda: [t * f for t, f in zip(leaves, (SHARP, 1.0, 1.0))]  # noqa: E731
+    f = {"joint": vc.joint_attention, "spatial": vc.spatial_attention, "temporal": vc.temporal_attention, "block": vc.parallel_block_attention}[branch]
+    with vc.saved_in_8bit(min_elements=1):
+        mine = scaled()
+        o = f(*mine, desc)
+    got = torch.autograd.grad(o, mine, do)
+    with torch.no_grad():
+        q, k, v = scaled()
+        each = []
+        for fwd, bwd in {"joint": [(vc.fwd, vc.bwd)], "spatial": [(vc.spatial_fwd, vc.spatial_bwd)], "temporal": [(vc.temporal_fwd, vc.temporal_bwd)],
+                         "block": [(vc.fwd, vc.bwd), (vc.spatial_fwd, vc.spatial_bwd), (vc.temporal_fwd, vc.temporal_bwd)]}[branch]:
+            # of the block the branches' own outputs are no results of an operation, and stay
+            oi, lse = fwd(q, k, v, desc)
+            each.append(bwd(q, k, _through(v), oi if branch == "block" else _through(oi), lse, do, desc))
+        want = each[0] if branch != "block" else [vc.branch_sum(desc, *g) for g in zip(*each)]
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_queries_keys_and_bias_of_packed_attention_stay():
+    import torch
+    vc = _vc()
+    T, H, D, NB, MD = 300, 2, 64, 64, 128
+    cu = torch.tensor([0, 200, 201, 300], dtype=torch.int32, device="cuda")
+    desc = vc.make_packed_desc(3, H, H, D, T, T, 200, 200, num_buckets=NB, max_distance=MD)
+    buckets = vc.relative_buckets(NB, MD)
+    leaves = _leaves(T, H, D) + _leaves(H, NB, n=1)
+    do = torch.randn((T, H, D), device="cuda").to(torch.bfloat16)
+    scaled = lambda: [t * f for t, f in zip(leaves, (SHARP, 1.0, 1.0, 4.0))]  # noqa: E731
+    with vc.saved_in_8bit(min_elements=1):
+        mine = scaled()
+        o = vc.packed_attention(*mine[:3], desc, cu, cu, bias=mine[3], buckets=buckets)
+    got = torch.autograd.grad(o, mine, do)
+    with torch.no_grad():
+        q, k, v, bias = scaled()
+        eo, lse = vc.packed_fwd(q, k, v, desc, cu, cu, bias=bias, buckets=buckets)
+        want = vc.packed_bwd(q, k, _through(v), _through(eo), lse, do, desc, cu, cu, bias=bias, buckets=buckets)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
