@@ -380,10 +380,32 @@ class _Whole(NamedTuple):
     version: int
 
 
+# Operations whose results are values of their operands: casts, copies, views, joined tensors.
+_MOVES = frozenset("%sBackward" % n for n in (
+    "ToCopy", "Clone", "Alias", "View", "UnsafeView", "ReshapeAlias", "T", "Transpose", "Permute", "Select", "Slice", "Split",
+    "SplitWithSizes", "Unbind", "Squeeze", "Unsqueeze", "Expand", "AsStrided", "Cat", "Stack"))
+
+
+def _of_leaves(t):
+    """Whether t is a leaf or holds the values of leaves in another type, order or place."""
+    t = t if t._base is None else t._base
+    open_, seen = [] if t.is_leaf else [t.grad_fn], set()
+    while open_:
+        f = open_.pop()
+        if f is None or f in seen or hasattr(f, "variable"):  # a constant, or a leaf's end of the graph
+            continue
+        seen.add(f)
+        if f.name().rstrip("0123456789") not in _MOVES:
+            return False
+        open_ += [g for g, _ in f.next_functions]
+    return True
+
+
 def saved_in_8bit(min_elements=1 << 16):
     """A context in which autograd keeps activations in 8 bits: contiguous tensors of bf16, of at least min_elements elements, two
     dimensions and 64 columns, that an operation saves for its backward are packed, and unpacked where the backward asks for
-    them. Leaves (parameters, inputs) and views of them stay as they are, for they are kept anyway, and so do tensors of 32 bits
+    them. Leaves (parameters, inputs) stay as they are, and so do casts, copies, views and joined forms of them (weights in bf16 of
+    parameters in 32 bits): an input's gradient is that of the weight itself. Weights that are computed otherwise are taken for activations. Tensors of 32 bits stay too
     (log-sum-exps, statistics). A tensor that several operations save is packed for each of them. Of an attention of this package v
     and o are packed; q, k and a bias stay, since the backward computes the probabilities again from them with the exact log-sum-exps.
     A fused attention of another origin that does the same does not belong in the context: it cannot be told from other operations here."""
@@ -391,7 +413,8 @@ def saved_in_8bit(min_elements=1 << 16):
 
     def pack(t):
         if (t.device.type != "cuda" or t.dtype is not torch.bfloat16 or t.dim() < 2 or
-                t.numel() < min_elements or hasattr(t, "_vc_save_whole") or (t if t._base is None else t._base).is_leaf or t.shape[-1] < 64 or not t.is_contiguous()):
+                t.numel() < min_elements or t.shape[-1] < 64 or not t.is_contiguous() or
+                hasattr(t, "_vc_save_whole") or _of_leaves(t)):
             return _Whole(t.detach(), t._version)  # a result that its operation saves would hold that operation, and itself through it
         return checkpoint_pack(t.detach())
 

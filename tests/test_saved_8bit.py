@@ -71,3 +71,21 @@ def test_changed_in_place_after_it_was_saved():
         y = u.exp() + 0
         y.mul_(3)
     assert torch.equal(torch.autograd.grad(y.sum(), x)[0], 6 * (2 * x.detach() + 1).exp())
+
+
+def test_which_tensors_are_of_leaves():
+    of = vc.blocks._of_leaves
+    w, v, x = (torch.randn((4, 6), requires_grad=True) for _ in range(3))
+    plain = torch.randn((4, 6))
+    low = w.to(torch.bfloat16)
+    for t in (w, plain, w.detach(), w.t(), w[1:], low, low.t().contiguous(), low.clone()[0], torch.cat([w, v]), torch.stack([w, plain]).unbind(0)[0],
+              torch.cat([w.t().to(torch.bfloat16), plain.to(torch.bfloat16).t()], 1).view(-1), w.diagonal(), low.unsqueeze(0).expand(2, 4, 6)):
+        assert of(t), t.grad_fn
+    changed = w.clone()
+    changed[0].mul_(2)
+    for t in (w * 2, (w * 2).to(torch.bfloat16), (x + 0).t(), torch.cat([w, v * 2]), w.t() @ v, changed, changed.view(-1)):
+        assert not of(t), t.grad_fn
+    many = w
+    for _ in range(40):  # 2^40 ways to the leaf
+        many = torch.cat([many[:1], many[:1]])
+    assert of(many)

@@ -67,3 +67,27 @@ def test_queries_keys_and_bias_of_packed_attention_stay():
         eo, lse = vc.packed_fwd(q, k, v, desc, cu, cu, bias=bias, buckets=buckets)
         want = vc.packed_bwd(q, k, _through(v), _through(eo), lse, do, desc, cu, cu, bias=bias, buckets=buckets)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("how", ["cast", "autocast", "columns", "joined", "one of several", "copied twice"])
+def test_weights_in_another_form_stay(how):
+    """bf16 copies of parameters in 32 bits, and joined, transposed or picked ones: the input's gradient is that of the weight itself, not of its 8
+    bits, and so are the products' others."""
+    import torch
+    vc = _vc()
+    new = lambda *s: torch.randn(s, device="cuda").requires_grad_(True)  # noqa: E731
+    wide, parts, many, x = new(256, 256), [new(256, 128), new(256, 128)], new(3, 256, 256), _leaves(300, 256, n=1)[0]
+    dy = torch.randn((300, 256), device="cuda").to(torch.bfloat16)
+    low = torch.bfloat16
+    form = {"cast": lambda: wide.to(low), "autocast": lambda: wide, "columns": lambda: wide.to(low).t().contiguous(),
+            "joined": lambda: torch.cat([p.to(low) for p in parts], 1), "one of several": lambda: many.to(low)[1],
+            "copied twice": lambda: wide.clone().to(low).view(128, 512).reshape(256, 256)}[how]
+
+    def product():
+        with torch.autocast("cuda", low, enabled=how == "autocast"):
+            return x @ form()
+
+    want = torch.autograd.grad(product(), x, dy)[0]
+    with vc.saved_in_8bit(min_elements=1):
+        y = product()
+    assert torch.equal(torch.autograd.grad(y, x, dy)[0], want)
