@@ -578,10 +578,10 @@ def temporal_bwd(q, k, v, o, lse, dout, desc, key_mask=None, ws=None):
 
 
 def _save_whole(*tensors):
-    """Marks tensors that an operation saves for its backward and that saved_in_8bit is to leave as they are: q, k and the bias of an
-    attention, whose probabilities the backward computes again with the exact log-sum-exps. From 8 bits, rows of sharp
-    probabilities would not add up to 1 (logits of a standard deviation of 4, 8, 16: sums of 0.91 to 1.13, 0.80 to 1.22, 0.66 to 1.45,
-    gradients off by 4, 8, 17%; with q and k as they are by 1.6, 2.2, 2.9%)."""
+    """Marks tensors that an operation saves for its backward and that saved_in_8bit is to leave as they are: the vectors of a
+    residual_norm; q, k and the bias of an attention, whose probabilities the backward computes again with the exact log-sum-exps. From
+    8 bits, rows of sharp probabilities would not add up to 1 (logits of a standard deviation of 4, 8, 16: sums of 0.91 to 1.13, 0.80
+    to 1.22, 0.66 to 1.45, gradients off by 4, 8, 17%; with q and k as they are by 1.6, 2.2, 2.9%)."""
     for t in tensors:
         if t is not None and not t.is_leaf:  # leaves stay anyway
             t._vc_save_whole = True

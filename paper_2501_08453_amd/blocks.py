@@ -9,8 +9,8 @@ from __future__ import annotations
 import ctypes
 from typing import NamedTuple
 
-from paper_2501_08453_amd import (JointAttnError, _call, _lib, _ptr, _stream, _workspace, vc_checkpoint_desc,
-                                  vc_embedding_desc, vc_residualnorm_desc)
+from paper_2501_08453_amd import (JointAttnError, _call, _lib, _ptr, _save_whole, _stream, _workspace,
+                                  vc_checkpoint_desc, vc_embedding_desc, vc_residualnorm_desc)
 from paper_2501_08453_amd.tower import _check_all, _row_stride, _ws_bytes
 
 NORMS = {None: 0, "layer": 1, "rms": 2}  # VC_NORM_*
@@ -408,6 +408,7 @@ def saved_in_8bit(min_elements=1 << 16):
     parameters in 32 bits): an input's gradient is that of the weight itself. Weights that are computed otherwise are taken for activations. Tensors of 32 bits stay too
     (log-sum-exps, statistics). A tensor that several operations save is packed for each of them. Of an attention of this package v
     and o are packed; q, k and a bias stay, since the backward computes the probabilities again from them with the exact log-sum-exps.
+    The vectors of a residual_norm stay, which are few and weigh every row.
     A fused attention of another origin that does the same does not belong in the context: it cannot be told from other operations here."""
     import torch
 
@@ -509,6 +510,7 @@ def _autograd_functions():
             kept = (s.h, s.a)
             if s.desc.checkpoint:
                 kept = tuple(t for k in kept for t in ((None, None) if k is None else (k.q, k.scales)))
+            _save_whole(gate, scale, shift, post_weight)
             ctx.save_for_backward(*kept, gate, scale, shift, post_weight, cu, lens, s.stats)
             ctx.desc, ctx.types = s.desc, (x.dtype, s.y_dtype)
             if a is None:  # h is x: the caller has it

@@ -91,3 +91,24 @@ def test_weights_in_another_form_stay(how):
     with vc.saved_in_8bit(min_elements=1):
         y = product()
     assert torch.equal(torch.autograd.grad(y, x, dy)[0], want)
+
+
+def test_vectors_of_the_samples_stay():
+    """gate, scale and shift of each sample, results of projections: the gradients of x and a are those of the vectors themselves; h, the
+    stream that the operation saves, is packed."""
+    import torch
+    vc = _vc()
+    rows, cols, S = 96, 256, 4
+    x, a, dh, dy = [t.detach() for t in _leaves(rows, cols, n=4)]
+    leaves, t = _leaves(cols, cols), _leaves(S, cols, n=1)[0].detach()
+    a.requires_grad_(True)
+    x.requires_grad_(True)
+    desc = vc.make_residual_desc(rows, cols, S)
+    with vc.saved_in_8bit(min_elements=1):
+        vec = [t @ w for w in leaves]
+        h, y = vc.residual_norm(x, a, desc, *vec)
+    got = torch.autograd.grad((h, y), [x, a] + vec, (dh, dy))
+    with torch.no_grad():
+        eh, ey, saved = vc.residual_norm_fwd(x, a, desc, *vec)
+        want = vc.residual_norm_bwd(dh, dy, saved._replace(h=_through(eh)))
+    assert torch.equal(h, eh) and torch.equal(y, ey) and all(torch.equal(p, q) for p, q in zip(got, want))
