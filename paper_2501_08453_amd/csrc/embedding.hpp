@@ -28,7 +28,7 @@ struct EmbeddingArgs {
 };
 
 constexpr int64_t kEmbeddingTokens = (int64_t)1 << 24;  // most tokens of a backward
-constexpr int64_t kEmbeddingVocab = (int64_t)1 << 27;   // most rows of a table: three passes of nine bits
+constexpr int64_t kEmbeddingVocab = (int64_t)1 << 27;   // most rows of a table: three passes of nine bits, of 2^27 itself (keys go up to it) four of seven
 struct EmbeddingPlan {
   int passes, digits, blocks, chunk, chunks;
 };
