@@ -537,7 +537,8 @@ vc_status vc_layernorm_bwd(const vc_layernorm_desc* desc,
  *    are read on the device only; nothing outside the tensors is read or written whatever they hold.
  *  - Rows of a slot behind its length get h = y = 0, dx = da = 0; what the inputs hold there has no effect. Rows
  *    outside every slot are left as they were, or with `clear_outside` written as those.
- *  - gate NULL: 1; scale NULL: e = 1; shift NULL: 0; post_weight NULL: 1. a NULL (a norm alone; c = 1, no
+ *  - gate NULL: 1; scale NULL: e = 1; shift NULL: 0; post_weight NULL: 1; gradients of vectors that are not given may be wanted all
+ *    the same, and lie as their stride says. a NULL (a norm alone; c = 1, no
  *    gate and no post_norm): h = x, written unless h is NULL. norm VC_NORM_NONE (the residual alone): no y.
  *  - With `checkpoint` the forward writes what its backward needs of h and a in 8 bits beside them (see
  *    vc_checkpoint_pack: h8, a8 int8 [rows, cols], scales fp32 [rows, ceil(cols / 128)]), and the backward takes these in

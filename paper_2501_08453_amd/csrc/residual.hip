@@ -591,9 +591,8 @@ __global__ __launch_bounds__(1024) void residual_shared_kernel(ResidualArgs a) {
 
 constexpr int kFewCols = 2048;
 // Whether a call reads and writes its rows past the caches, as these are more than the last one's 256 MiB: the backward, and a forward
-// that keeps 8 bits, which then stay there for the backward. 57,856 x 1,536: backward 217 us so and 229 otherwise, with 8 bits 194
-// and 228, their forward 191 and 198; a forward without them 149 and 154
-// by itself, but 372 and 343 with its backward behind it.
+// that keeps 8 bits, which then stay there for the backward. 57,856 x 1,536: backward 208 us so and 230 otherwise, with 8 bits 197
+// and 230, their forward 198 and 203; a forward without them 147 so and 142 otherwise, and its backward 221 behind it instead of 208.
 bool once_of(const ResidualArgs& a, bool backward) {
   const int64_t bytes = (int64_t)a.rows * a.cols * ((a.x_f32 ? 4 : 2) + (a.y_f32 ? 4 : 2)) * (backward ? 3 : 2);
   return (backward || a.h8 || a.a8) && bytes > ((int64_t)256 << 20);

@@ -9,8 +9,8 @@ ratio is recomputed (Sec. VI-D, Tab. offload). For the attention of a parallel b
 saved activations are what each branch's backward needs besides q, k, v: its O and LSE
 (the joint, spatial and temporal branches; the branch sum needs nothing).
 
-A fourth strategy keeps the layers' O in 8 bits on the device (checkpoint_pack; LSE as it is): 1 + 1/32
-bytes an element instead of 2, and D of their backward from values off by up to half a step of a 127th of the
+A fourth strategy keeps the layers' O in 8 bits on the device (checkpoint_pack; LSE as it is): a scale for each
+head's row of up to 128 columns, so 1 + 1/32 bytes an element instead of 2 with heads of 128 and 1 + 1/16 with heads of 64, and D of their backward from values off by up to half a step of a 127th of the
 largest of each 128.
 
 `plan` assigns every layer keep / recompute / offload / pack; `BlockStack` runs the block's
