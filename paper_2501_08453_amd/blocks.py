@@ -392,7 +392,7 @@ def _of_leaves(t):
     open_, seen = [] if t.is_leaf else [t.grad_fn], set()
     while open_:
         f = open_.pop()
-        if f is None or f in seen or hasattr(f, "variable"):  # a constant, or a leaf's end of the graph
+        if f is None or f in seen or f.name() == "torch::autograd::AccumulateGrad":  # a constant, or a leaf's end of the graph
             continue
         seen.add(f)
         if f.name().rstrip("0123456789") not in _MOVES:
@@ -409,13 +409,14 @@ def saved_in_8bit(min_elements=1 << 16):
     (log-sum-exps, statistics). A tensor that several operations save is packed for each of them. Of an attention of this package v
     and o are packed; q, k and a bias stay, since the backward computes the probabilities again from them with the exact log-sum-exps.
     The vectors of a residual_norm stay, which are few and weigh every row.
-    A fused attention of another origin that does the same does not belong in the context: it cannot be told from other operations here."""
+    Results of log_softmax (cross_entropy) stay, of which the backward takes exponentials. Other operations whose backward takes exponentials
+    of what they saved (a fused attention of another origin, logsumexp) cannot be told from the rest here and do not belong in the context."""
     import torch
 
     def pack(t):
         if (t.device.type != "cuda" or t.dtype is not torch.bfloat16 or t.dim() < 2 or
                 t.numel() < min_elements or t.shape[-1] < 64 or not t.is_contiguous() or
-                hasattr(t, "_vc_save_whole") or _of_leaves(t)):
+                hasattr(t, "_vc_save_whole") or _of_leaves(t) or "LogSoftmax" in (t.grad_fn.name() if t.grad_fn else "")):
             return _Whole(t.detach(), t._version)  # a result that its operation saves would hold that operation, and itself through it
         return checkpoint_pack(t.detach())
 

@@ -112,3 +112,37 @@ def test_vectors_of_the_samples_stay():
         eh, ey, saved = vc.residual_norm_fwd(x, a, desc, *vec)
         want = vc.residual_norm_bwd(dh, dy, saved._replace(h=_through(eh)))
     assert torch.equal(h, eh) and torch.equal(y, ey) and all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+def test_logarithms_of_probabilities_stay():
+    """The backward of log_softmax takes exponentials of what it saved: from 8 bits, steps of a 127th of the largest of 128 logarithms
+    are ten percent of a probability and more, and of a target whose probability is near 1 nothing is left."""
+    import torch
+    vc = _vc()
+    x = _leaves(256, 1024, n=1)[0]
+    target = torch.arange(256, device="cuda")
+    with torch.no_grad():
+        x[target, target] += 10.0
+
+    def loss():
+        return torch.nn.functional.cross_entropy(x * 1.5, target)
+
+    want = torch.autograd.grad(loss(), x)[0]
+    with vc.saved_in_8bit(min_elements=1):
+        out = loss()
+    assert torch.equal(torch.autograd.grad(out, x)[0], want)
+
+
+def test_views_without_a_history_of_their_own():
+    """A view of an activation that is taken without gradients: packed as the activation is, and a constant to autograd."""
+    import torch
+    vc = _vc()
+    x, w = _leaves(128, 256, n=2)
+    y = x * 1.5
+    with torch.no_grad():
+        part = y.view(256, 128)
+    scale = w.view(256, 128)
+    for context, kept in ((torch.enable_grad, part), (lambda: vc.saved_in_8bit(min_elements=1), _through(part))):
+        with context():
+            out = part * scale
+        assert torch.equal(torch.autograd.grad(out.float().sum(), w)[0], kept.view(128, 256))
